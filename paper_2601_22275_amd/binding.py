@@ -2,7 +2,7 @@
 
 Every function takes torch CUDA tensors for device memory, hands their raw
 pointers and the current HIP stream to the C ABI declared in
-``include/vmonarch.h`` and raises ``VMonarchError`` on a non-zero return code.
+``include/vmonarch.h`` and ``include/vmonarch_sequence.h`` and raises ``VMonarchError`` on a non-zero return code.
 No arithmetic of the method happens on the Python side, and there is no
 fallback: if the shared library has not been built, importing this module's
 library handle raises.
@@ -10,6 +10,7 @@ library handle raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from ctypes import c_char_p, c_float, c_int, c_size_t, c_void_p
 
@@ -36,6 +37,10 @@ EXPORTS = [
     "vmonarch_set_flash_variant", "vmonarch_get_flash_variant",
     "vmonarch_options_init", "vmonarch_attention_ex", "vmonarch_attention_ex_f32",
     "vmonarch_recompute_tokens", "vmonarch_recompute_tokens_f32",
+    "vmonarch_rotary_init", "vmonarch_rotary_scale", "vmonarch_rotary", "vmonarch_rotary_f32",
+    "vmonarch_packed_attention", "vmonarch_packed_attention_f32", "vmonarch_packed_attention_bwd_workspace_bytes",
+    "vmonarch_packed_attention_bwd", "vmonarch_packed_attention_bwd_f32", "vmonarch_paged_append", "vmonarch_paged_append_f32",
+    "vmonarch_paged_attention_workspace_bytes", "vmonarch_paged_attention", "vmonarch_paged_attention_f32",
 ]
 
 
@@ -48,6 +53,30 @@ class Options(ctypes.Structure):
     _fields_ = [("struct_bytes", ctypes.c_uint32), ("cr_min", c_float), ("entropy_mode", c_int),
                 ("fused_apply", c_int), ("flash_variant", c_int), ("cr_control", c_int), ("cl_control", c_int),
                 ("cl_value", c_float), ("workspace", c_void_p), ("workspace_bytes", c_size_t)]
+
+
+ROTARY_HALF = 0
+ROTARY_INTERLEAVED = 1
+ROTARY_MAX_PAIRS = 128
+
+
+class Tokens(ctypes.Structure):
+    """vmonarch_tokens of include/vmonarch_sequence.h: a strided token tensor."""
+    _fields_ = [("data", c_void_p), ("token_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong)]
+
+
+class RotaryPlan(ctypes.Structure):
+    """vmonarch_rotary_plan: which pairs of a head turn how fast."""
+    _fields_ = [("struct_bytes", ctypes.c_uint32), ("layout", c_int), ("axes", c_int), ("axis_pairs", c_int * 3),
+                ("amplitude", ctypes.c_double), ("frequency", ctypes.c_double * ROTARY_MAX_PAIRS)]
+
+
+class Cache(ctypes.Structure):
+    """vmonarch_cache: keys and values in pages, the table of pages and the lengths of the sequences."""
+    _fields_ = [("k", c_void_p), ("v", c_void_p)] + [(n, ctypes.c_longlong) for n in (
+        "k_page_stride", "k_token_stride", "k_head_stride", "v_page_stride", "v_token_stride", "v_head_stride")] + [
+        ("n_pages", c_int), ("page_size", c_int), ("table", c_void_p), ("table_stride", ctypes.c_longlong), ("table_width", c_int),
+        ("lengths", c_void_p)]
 
 
 _lib = None
@@ -102,6 +131,22 @@ def lib() -> ctypes.CDLL:
         L.vmonarch_index_maps.argtypes = [c_int, c_int, c_int, c_void_p, c_void_p]
         L.vmonarch_permute_tokens.argtypes = [c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int, c_int, c_int,
                                               c_void_p]
+        plan, n = ctypes.POINTER(RotaryPlan), ctypes.c_longlong
+        L.vmonarch_rotary_init.argtypes = [plan, c_int, ctypes.c_double, c_int, c_void_p]
+        L.vmonarch_rotary_scale.argtypes = [plan] + [ctypes.c_double] * 4
+        for suffix in ("", "_f32"):
+            getattr(L, "vmonarch_rotary" + suffix).argtypes = [c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_int, n, c_int, c_void_p, n, c_void_p,
+                                                               c_int, c_void_p]
+            getattr(L, "vmonarch_packed_attention" + suffix).argtypes = [c_void_p] * 7 + [c_int, n, n, c_int, c_int, c_int, c_float, c_int, c_void_p]
+            getattr(L, "vmonarch_packed_attention_bwd" + suffix).argtypes = [c_void_p] * 11 + [c_int, n, n, c_int, c_int, c_int, c_float, c_int,
+                                                                                              c_void_p, c_size_t, c_void_p]
+            getattr(L, "vmonarch_paged_append" + suffix).argtypes = [c_void_p] * 4 + [c_int, n, c_int, c_int, c_void_p, c_void_p, n, c_void_p]
+            getattr(L, "vmonarch_paged_attention" + suffix).argtypes = [c_void_p] * 4 + [c_int, n, c_int, c_int, c_int, c_float, c_int, c_void_p,
+                                                                                        c_size_t, c_void_p]
+        L.vmonarch_packed_attention_bwd_workspace_bytes.restype = c_size_t
+        L.vmonarch_packed_attention_bwd_workspace_bytes.argtypes = [n, c_int]
+        L.vmonarch_paged_attention_workspace_bytes.restype = c_size_t
+        L.vmonarch_paged_attention_workspace_bytes.argtypes = [c_void_p, c_int, n, c_int, c_int, c_int]
         _lib = L
     return _lib
 
@@ -364,4 +409,179 @@ def permute_tokens(x, T, Hs, Ws, to_position_major=True, out=None):
         out = torch.empty_like(x)
     _check(lib().vmonarch_permute_tokens(_ptr(x), _ptr(out), B, heads, T, Hs, Ws, d * x.element_size(),
                                          int(bool(to_position_major)), _stream()))
+    return out
+
+
+# ---- token sequences (include/vmonarch_sequence.h) ---------------------------------------------------------------------------
+#
+# Token tensors are [tokens, heads, d] views with adjacent channels and any other strides.  Calls run on the tensors' device, on its
+# current stream; outputs and workspaces that the caller does not bring come from torch's allocator.
+
+
+def _sizes(name, x):
+    if x.dim() != 3:
+        raise VMonarchError(f"{name}: expected [tokens, heads, d], got {tuple(x.shape)}")
+    return x.shape
+
+
+def _tokens(name, x, like=None):
+    """The descriptor of token tensor x, checked against the type, device and head size of `like`."""
+    _sizes(name, x)
+    t, h, c = x.stride()
+    if (c != 1 and x.shape[2] > 1) or not x.is_cuda:
+        raise VMonarchError(f"{name}: a CUDA tensor with adjacent channels is needed")
+    if like is not None and (x.dtype != like.dtype or x.device != like.device or x.shape[2] != like.shape[2]):
+        raise VMonarchError(f"{name}: type, device or head size differ from the other tensors'")
+    return Tokens(x.data_ptr(), t, h)
+
+
+def _int32(name, x, like, shape=None):
+    if x.dtype != torch.int32 or x.device != like.device or not x.is_contiguous():
+        raise VMonarchError(f"{name}: a contiguous int32 tensor on the other tensors' device is needed")
+    if shape is not None and tuple(x.shape) != shape:
+        raise VMonarchError(f"{name}: expected shape {shape}, got {tuple(x.shape)}")
+    return x.data_ptr()
+
+
+def _same_shape(name, x, y):
+    if x.shape != y.shape:
+        raise VMonarchError(f"{name}: expected shape {tuple(y.shape)}, got {tuple(x.shape)}")
+
+
+def _run(name, like, *args):
+    """Calls an entry point on the current stream of `like`'s device."""
+    fn = getattr(lib(), name + _suffix(like))
+    dev = like.device.index
+    if dev == torch.cuda.current_device():
+        _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+
+
+def rotary_plan(axis_pairs, base=10000.0, interleaved=False, factor=1.0, context=0.0, low_turns=0.0, high_turns=0.0, amplitude=1.0) -> RotaryPlan:
+    """Rotary positions: axis_pairs[a] pairs turn with the position on axis a (one to three axes), their frequencies base^(-i / n) stretched
+    for contexts `factor` times as long: all pairs alike (context = 0), or by band (see vmonarch_rotary_scale)."""
+    plan = RotaryPlan()
+    n = (c_int * len(axis_pairs))(*axis_pairs)
+    _check(lib().vmonarch_rotary_init(ctypes.byref(plan), ROTARY_INTERLEAVED if interleaved else ROTARY_HALF, base, len(axis_pairs), n))
+    if factor != 1.0:
+        _check(lib().vmonarch_rotary_scale(ctypes.byref(plan), factor, context, low_turns, high_turns))
+    plan.amplitude = amplitude
+    return plan
+
+
+def rotary(q, k, positions, plan: RotaryPlan, backward=False, q_out=None, k_out=None):
+    """Turns q and k ([tokens, heads, d]; k may be None) at positions (int32 [axes, tokens], or [tokens] for one axis); backward: gradients of the
+    turned tensors to those of q and k.  q_out / k_out may be q / k themselves.  Returns (q_out, k_out)."""
+    n, heads, d = _sizes("q", q)
+    q_out = torch.empty_like(q) if q_out is None else q_out
+    dq, dqo, dk, dko, heads_k = _tokens("q", q), _tokens("q_out", q_out, q), None, None, 0
+    _same_shape("q_out", q_out, q)
+    if k is not None:
+        k_out = torch.empty_like(k) if k_out is None else k_out
+        dk, dko, heads_k = _tokens("k", k, q), _tokens("k_out", k_out, q), k.shape[1]
+        _same_shape("k_out", k_out, k)
+        if k.shape[0] != n:
+            raise VMonarchError("k: as many tokens as q are needed")
+        dk, dko = ctypes.byref(dk), ctypes.byref(dko)
+    elif k_out is not None:
+        raise VMonarchError("k_out without k")
+    if positions.dim() == 1:
+        positions = positions[None]
+    at = _int32("positions", positions, q, (plan.axes, n))
+    _run("vmonarch_rotary", q, ctypes.byref(dq), ctypes.byref(dqo), heads, dk, dko, heads_k, n, d, at, n, ctypes.byref(plan), int(bool(backward)))
+    return q_out, k_out
+
+
+def packed_attention(q, k, v, q_starts, k_starts=None, causal=True, scale=None, out=None, lse=False):
+    """Attention over packed sequences: q [tokens_q, heads_q, d]; k, v [tokens_k, heads_kv, d]; q_starts / k_starts int32 [n_seqs + 1] (k_starts None:
+    q_starts).  scale defaults to 1 / sqrt(d).  Returns out, or (out, lse) with lse float32 [heads_q, tokens_q] for packed_attention_bwd.
+    Rows of no sequence are not written: bring a cleared `out` where a padded batch's tail is read later."""
+    nq, heads, d = _sizes("q", q)
+    k_starts = q_starts if k_starts is None else k_starts
+    out = torch.empty((nq, heads, d), dtype=q.dtype, device=q.device) if out is None else out
+    _same_shape("out", out, q)
+    _same_shape("v", v, k)
+    stat = torch.empty((heads, nq), dtype=torch.float32, device=q.device) if lse else None
+    n = q_starts.numel()
+    a, b, c, o = _tokens("q", q), _tokens("k", k, q), _tokens("v", v, q), _tokens("out", out, q)
+    _run("vmonarch_packed_attention", q, ctypes.byref(a), ctypes.byref(b), ctypes.byref(c), ctypes.byref(o), stat.data_ptr() if lse else None,
+         _int32("q_starts", q_starts, q, (n,)), _int32("k_starts", k_starts, q, (n,)), n - 1, nq, k.shape[0], heads, k.shape[1], d,
+         1.0 / math.sqrt(d) if scale is None else scale, int(bool(causal)))
+    return (out, stat) if lse else out
+
+
+def packed_attention_bwd(q, k, v, out, d_out, lse, q_starts, k_starts=None, causal=True, scale=None, dq=None, dk=None, dv=None, workspace=None):
+    """Gradients (dq, dk, dv) of packed_attention from its out and lse.  Rows of no sequence are not written (see there)."""
+    nq, heads, d = _sizes("q", q)
+    k_starts = q_starts if k_starts is None else k_starts
+    dq = torch.empty((nq, heads, d), dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
+    dv = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dv is None else dv
+    for name, x, y in (("v", v, k), ("out", out, q), ("d_out", d_out, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
+        _same_shape(name, x, y)
+    if lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous() or tuple(lse.shape) != (heads, nq):
+        raise VMonarchError("lse: the log-sum-exp of packed_attention is needed, float32 [heads_q, tokens_q]")
+    if workspace is None:
+        workspace = torch.empty(lib().vmonarch_packed_attention_bwd_workspace_bytes(nq, heads), dtype=torch.uint8, device=q.device)
+    n = q_starts.numel()
+    x = [_tokens(name, t, q) for name, t in (("q", q), ("k", k), ("v", v), ("out", out), ("d_out", d_out), ("dq", dq), ("dk", dk), ("dv", dv))]
+    p = [ctypes.byref(t) for t in x]
+    size = workspace.numel() * workspace.element_size()
+    _run("vmonarch_packed_attention_bwd", q, *p[:5], lse.data_ptr(), *p[5:], _int32("q_starts", q_starts, q, (n,)),
+         _int32("k_starts", k_starts, q, (n,)), n - 1, nq, k.shape[0], heads, k.shape[1], d, 1.0 / math.sqrt(d) if scale is None else scale,
+         int(bool(causal)), workspace.data_ptr() if size else None, size)
+    return dq, dk, dv
+
+
+def _cache(cache_k, cache_v, table, lengths, like, n_seqs):
+    """The descriptor of a cache: cache_k, cache_v [pages, page_size, heads_kv, d] with adjacent channels, table int32 [n_seqs, width]."""
+    _same_shape("cache_v", cache_v, cache_k)
+    for name, x in (("cache_k", cache_k), ("cache_v", cache_v)):
+        if x.dim() != 4 or x.dtype != like.dtype or x.device != like.device or x.shape[3] != like.shape[2] or (x.stride(3) != 1 and x.shape[3] > 1):
+            raise VMonarchError(f"{name}: expected [pages, page_size, heads, d] with adjacent channels, of the other tensors' type, device and head size")
+    if table.dtype != torch.int32 or table.device != like.device or table.dim() != 2 or table.shape[0] != n_seqs or (table.stride(1) != 1 and table.shape[1] > 1):
+        raise VMonarchError("table: expected int32 [n_seqs, pages of the longest] on the other tensors' device")
+    ks, vs = cache_k.stride(), cache_v.stride()
+    return Cache(cache_k.data_ptr(), cache_v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], cache_k.shape[0], cache_k.shape[1], table.data_ptr(),
+                 table.stride(0), table.shape[1], _int32("lengths", lengths, like, (n_seqs,)))
+
+
+def paged_append(k, v, cache_k, cache_v, table, q_starts, lengths, plan: RotaryPlan = None, positions=None):
+    """Writes each sequence's chunk of new tokens (k, v [tokens, heads_kv, d], cut by q_starts) into the last slots of its lengths[s] tokens in the
+    pages; with a plan keys are turned on the way, at `positions` or at the tokens' positions in their sequence."""
+    n = q_starts.numel() - 1
+    _same_shape("v", v, k)
+    a, b, c = _tokens("k", k), _tokens("v", v, k), _cache(cache_k, cache_v, table, lengths, k, n)
+    if cache_k.shape[2] != k.shape[1]:
+        raise VMonarchError("cache_k: as many heads as k are needed")
+    at = None
+    if positions is not None:
+        if plan is None:
+            raise VMonarchError("positions without a plan")
+        positions = positions[None] if positions.dim() == 1 else positions
+        at = _int32("positions", positions, k, (plan.axes, k.shape[0]))
+    _run("vmonarch_paged_append", k, ctypes.byref(a), ctypes.byref(b), ctypes.byref(c), _int32("q_starts", q_starts, k, (n + 1,)), n, k.shape[0],
+         k.shape[1], k.shape[2], None if plan is None else ctypes.byref(plan), at, k.shape[0])
+
+
+def paged_attention(q, cache_k, cache_v, table, q_starts, lengths, causal=True, scale=None, out=None, workspace=None):
+    """Attention of each sequence's chunk of new tokens (q [tokens, heads_q, d], cut by q_starts) over its lengths[s] tokens in the pages, the chunk's
+    own included.  Rows of no sequence are not written (see packed_attention)."""
+    nq, heads, d = _sizes("q", q)
+    n = q_starts.numel() - 1
+    out = torch.empty((nq, heads, d), dtype=q.dtype, device=q.device) if out is None else out
+    _same_shape("out", out, q)
+    a, o, c = _tokens("q", q), _tokens("out", out, q), _cache(cache_k, cache_v, table, lengths, q, n)
+    kv = cache_k.shape[2]
+    size = 0
+    if workspace is None:
+        size = lib().vmonarch_paged_attention_workspace_bytes(ctypes.byref(c), n, nq, heads, kv, d)
+        if size:
+            workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+    else:
+        size = workspace.numel() * workspace.element_size()
+    _run("vmonarch_paged_attention", q, ctypes.byref(a), ctypes.byref(c), ctypes.byref(o), _int32("q_starts", q_starts, q, (n + 1,)), n, nq, heads, kv, d,
+         1.0 / math.sqrt(d) if scale is None else scale, int(bool(causal)), workspace.data_ptr() if size else None, size)
     return out

@@ -14,6 +14,7 @@
 #include <cmath>
 
 #include "common.h"
+#include "seq.h"
 
 using namespace vm;
 
@@ -211,6 +212,24 @@ void* get_workspace(size_t bytes, int* err, void* call_ws = nullptr, size_t call
   }
   return g_arena[dev];
 }
+
+}  // namespace
+
+// For the other units with C entry points (seq.h)
+namespace vm {
+int api_fail(int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_err, sizeof(g_err), fmt, ap);
+  va_end(ap);
+  return code;
+}
+void* api_workspace(size_t bytes, int* err, void* call_ws, size_t call_ws_bytes, hipStream_t st) {
+  return get_workspace(bytes, err, call_ws, call_ws_bytes, st);
+}
+}  // namespace vm
+
+namespace {
 
 // Settings of one call: the process-wide defaults (the setters above write them), or a caller's vmonarch_options.
 struct Settings {

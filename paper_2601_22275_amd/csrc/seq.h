@@ -1,0 +1,137 @@
+// Declarations shared by the token-sequence units (rotary.hip, seq_*.hip; not part of the ABI).
+#pragma once
+#include "../../include/vmonarch_sequence.h"
+#include "common.h"
+
+namespace vm {
+
+// api.hip: the library's error text and workspaces
+int api_fail(int code, const char* fmt, ...);
+void* api_workspace(size_t bytes, int* err, void* call_ws, size_t call_ws_bytes, hipStream_t st);
+
+// A strided token tensor on the device
+template <typename E>
+struct Rows {
+  E* p;
+  long long t, h;  // elements between tokens, between heads
+};
+
+// Keys or values: packed (page_size 0), or in pages
+template <typename E>
+struct KeyRows {
+  const E* p;
+  long long t, h, page;
+};
+
+// One attention problem as the kernels see it.  Query rows are PACKED: row r of a sequence and key head is token r / group of it, query
+// head kv_head * group + r % group, so that the heads that share keys fill a tile together, single tokens as well as prompts.
+template <typename E>
+struct SeqParams {
+  Rows<const E> q;
+  KeyRows<E> k, v;
+  Rows<E> out;
+  float* lse;           // [heads_q][tokens_q], or null
+  const int* q_starts;
+  const int* k_starts;  // packed keys
+  const int* lengths;   // keys in pages
+  const int* table;
+  long long table_stride;
+  int table_width, page_size, n_pages;  // page_size 0: packed keys
+  int n_seqs;
+  int tokens_q, tokens_k;
+  int heads_kv, group, d;
+  int causal;
+  int aligned;          // rows on 16-byte boundaries, d a multiple of 16 bytes
+  float scale;
+  // backward
+  Rows<const E> o, d_out;
+  Rows<E> dq, dk, dv;
+  float* delta;         // d_out . out per row, [heads_q][tokens_q]
+  // ranges of keys (seq_paged.hip)
+  float* part_o;
+  float* part_s;
+  int ranges;
+};
+
+// ---- device: sequences --------------------------------------------------------------------------------------------------------
+struct Span {
+  int seq, tile;     // tile of `BM` packed rows (keys: group 1) within the sequence
+  int begin, count;  // the sequence's tokens
+};
+
+// Start of sequence s, kept inside the tensor and in order whatever the array holds
+__device__ __forceinline__ int start_of(const int* starts, int s, int tokens) { return min(max(starts[s], 0), tokens); }
+
+// Tiles of BM rows (tokens * rows_per_token) of all sequences in one row of workgroups.  Sequence s owns tiles f(s) .. f(s+1) - 1 with
+// f(s) = floor(starts[s] rows_per_token / BM) + s: at least the ceil(rows / BM) it needs, so the host can launch f(n) =
+// floor(tokens rows_per_token / BM) + n of them without seeing the lengths.  The sequence of tile `t` is found by all lanes of a wave at once.
+__device__ __forceinline__ Span find_tile(const int* starts, int n_seqs, int tokens, int rows_per_token, int BM, int t) {
+  const int lane = threadIdx.x & 63;
+  int s = 0;
+  for (int base = 0; base < n_seqs; base += 64) {
+    const int i = base + lane;
+    const bool at_or_before = i < n_seqs && (long long)start_of(starts, i, tokens) * rows_per_token / BM + i <= t;
+    const unsigned long long b = __ballot(at_or_before);
+    if (b == 0) break;
+    s = base + 63 - __builtin_clzll(b);
+    if (s != base + 63) break;
+  }
+  s = __builtin_amdgcn_readfirstlane(s);
+  Span w;
+  w.seq = s;
+  w.begin = start_of(starts, s, tokens);
+  w.count = max(start_of(starts, s + 1, tokens) - w.begin, 0);
+  w.tile = t - (int)((long long)w.begin * rows_per_token / BM + s);
+  if (w.tile < 0) w.tile = w.count = 0;  // tokens in front of the first sequence
+  return w;
+}
+
+// Upper bound of the tiles of all sequences (see find_tile)
+inline long long tile_bound(long long tokens, int rows_per_token, int BM, int n_seqs) { return tokens * rows_per_token / BM + n_seqs; }
+
+// Keys of sequence s: where they begin (packed) and how many there are
+template <typename E>
+__device__ __forceinline__ int keys_of(const SeqParams<E>& P, int s, int* begin) {
+  if (P.page_size > 0) {
+    *begin = 0;
+    const long long room = (long long)P.table_width * P.page_size;
+    return (int)min((long long)max(P.lengths[s], 0), room);
+  }
+  *begin = start_of(P.k_starts, s, P.tokens_k);
+  return max(start_of(P.k_starts, s + 1, P.tokens_k) - *begin, 0);
+}
+
+// ---- launchers (host) -----------------------------------------------------------------------------------------------------------
+struct RotaryParams {
+  const void* in[2];   // q, k (append: k, v)
+  void* out[2];
+  long long in_t[2], in_h[2], out_t[2], out_h[2], out_page[2];
+  int heads[2];
+  int turned[2];       // pairs turned in tensor 0 / 1 (append: values pass through)
+  int tokens, d;
+  const int* positions;  // [axes][tokens]; null: the position in the sequence (append)
+  long long axis_stride;
+  int axis_end[3];     // pairs below this one belong to the axis
+  int interleaved;
+  float amplitude;
+  float sign;          // of the sine
+  // append
+  const int* starts;
+  const int* lengths;
+  const int* table;
+  long long table_stride;
+  int table_width, page_size, n_pages, n_seqs;
+};
+struct RotaryTurns {
+  double per_position[VMONARCH_ROTARY_MAX_PAIRS];  // full turns: frequency / 2 pi
+};
+// rotary.hip; elem_bytes 2: bf16, 4: float32; wide: rows in 16-byte pieces
+hipError_t launch_rotary(const RotaryParams& P, const RotaryTurns& F, int elem_bytes, bool wide, hipStream_t st);
+
+// seq_general.hip : any d <= 256, any strides, on the fp32 matrix units
+template <typename E>
+hipError_t launch_seq_attention_general(const SeqParams<E>& P, hipStream_t st);
+template <typename E>
+hipError_t launch_seq_attention_bwd_general(const SeqParams<E>& P, hipStream_t st);
+
+}  // namespace vm
