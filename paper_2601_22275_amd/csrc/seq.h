@@ -2,6 +2,7 @@
 #pragma once
 #include "../../include/vmonarch_sequence.h"
 #include "common.h"
+#include <stdlib.h>
 
 namespace vm {
 
@@ -52,6 +53,9 @@ struct SeqParams {
   float* part_s;
   int ranges;
 };
+
+// Backward, bf16: rows of queries whose workgroup sees at most this many keys sum D over them instead of reading it off the stored output
+constexpr int kSeqExactKeys = 256;
 
 // ---- device: sequences --------------------------------------------------------------------------------------------------------
 struct Span {
@@ -127,6 +131,12 @@ struct RotaryTurns {
 };
 // rotary.hip; elem_bytes 2: bf16, 4: float32; wide: rows in 16-byte pieces
 hipError_t launch_rotary(const RotaryParams& P, const RotaryTurns& F, int elem_bytes, bool wide, hipStream_t st);
+
+// seq_mfma.hip : bf16, aligned rows, d <= D (compiled for D = 64 and 128)
+template <int D>
+hipError_t launch_seq_attention_mfma(const SeqParams<bf16_t>& P, hipStream_t st);
+// Two 32-row query tiles per wave, or one
+inline bool seq_two_tiles(const SeqParams<bf16_t>& P) { return getenv("VM_TWO") ? atoi(getenv("VM_TWO")) : 0; }
 
 // seq_general.hip : any d <= 256, any strides, on the fp32 matrix units
 template <typename E>

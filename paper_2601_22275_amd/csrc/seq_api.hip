@@ -205,6 +205,14 @@ int append_impl(const vmonarch_tokens* k, const vmonarch_tokens* v, const vmonar
   return hip_result(launch_rotary(P, F, (int)elem, c.aligned && wide_pieces(P.interleaved, pairs, d, elem), as_stream(stream)), "paged_append launch");
 }
 
+template <typename E>
+hipError_t launch_attention(const SeqParams<E>& P, hipStream_t st) {
+  if constexpr (sizeof(E) == 2) {
+    if (P.aligned && P.d <= 128) return P.d <= 64 ? launch_seq_attention_mfma<64>(P, st) : launch_seq_attention_mfma<128>(P, st);
+  }
+  return launch_seq_attention_general<E>(P, st);
+}
+
 // ---- attention ------------------------------------------------------------------------------------------------------------------
 template <typename E>
 int packed_impl(const vmonarch_tokens* q, const vmonarch_tokens* k, const vmonarch_tokens* v, const vmonarch_tokens* out, float* lse,
@@ -231,7 +239,7 @@ int packed_impl(const vmonarch_tokens* q, const vmonarch_tokens* k, const vmonar
   P.heads_kv = heads_kv; P.group = heads_q / heads_kv; P.d = d;
   P.causal = causal != 0; P.scale = scale;
   P.aligned = c.aligned && d % (16 / (int)sizeof(E)) == 0;
-  return hip_result(launch_seq_attention_general<E>(P, as_stream(stream)), "packed_attention launch");
+  return hip_result(launch_attention<E>(P, as_stream(stream)), "packed_attention launch");
 }
 
 template <typename E>
@@ -305,7 +313,7 @@ int paged_impl(const vmonarch_tokens* q, const vmonarch_cache* cache, const vmon
   P.heads_kv = heads_kv; P.group = heads_q / heads_kv; P.d = d;
   P.causal = causal != 0; P.scale = scale;
   P.aligned = c.aligned && d % (16 / (int)sizeof(E)) == 0;
-  return hip_result(launch_seq_attention_general<E>(P, as_stream(stream)), "paged_attention launch");
+  return hip_result(launch_attention<E>(P, as_stream(stream)), "paged_attention launch");
 }
 
 }  // namespace

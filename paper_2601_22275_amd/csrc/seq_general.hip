@@ -147,7 +147,6 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
       if (ovalid) {
         const long long at = stat_of(orow);
         o_lse = P.lse[at] * LOG2E;
-        if (g == 0) P.delta[at] = o_delta;
       }
       if (o_lse == -INFINITY) o_lse = INFINITY;  // no weight anywhere
     }
@@ -194,6 +193,12 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
       for (int ct = 0; ct < 4; ++ct) acc[x][c][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
 
+  // d_out . out from the stored rows carries their rounding, which the difference dP - D does not forgive where a row's weight sits on a few
+  // keys (on one: dP - D is zero).  Rows of bf16 that see few keys get D = sum_j P dP in a round of its own.
+  const bool exact = MODE == GRAD_Q && sizeof(E) == 2 && s1 <= kSeqExactKeys;
+  for (int round = exact ? 0 : 1; round < 2; ++round) {
+  if (MODE == GRAD_Q && exact && round == 0) o_delta = 0.f;
+  float d_sum = 0.f;
   if (ntiles > 0) fetch(0);
   for (int tile = 0; tile < ntiles; ++tile) {
     const long long base = s0 + (long long)tile * BN;
@@ -243,7 +248,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
         }
       }
     }
-    float p[2][4], ds[2][4];
+    float p[2][4], ds[2][4], keep = 1.f;
     unsigned sees = 0;  // bit 4 kb + r
     if (MODE == FORWARD) {
       float top = -INFINITY;
@@ -262,18 +267,16 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
       const float ref = m2 == -INFINITY ? 0.f : m2;
       const float alpha = __builtin_amdgcn_exp2f(m - ref);
       m = m2;
-      l *= alpha;
+      float part = 0.f;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           p[kb][r] = __builtin_amdgcn_exp2f(s[kb][r] - ref);
-          l += p[kb][r];
+          part += p[kb][r];
         }
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int ct = 0; ct < 4; ++ct) acc[0][c][ct] *= alpha;
+      l = l * alpha + part;
+      keep = alpha;
     } else {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -294,9 +297,23 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
           }
           p[kb][r] = v ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][r], sc, -lse2)) : 0.f;
           ds[kb][r] = v ? p[kb][r] * (dp[kb][r] - delta) : 0.f;
+          if (MODE == GRAD_Q) d_sum += ds[kb][r];
         }
+      if (MODE == GRAD_Q && round == 0) {
+        __syncthreads();
+        continue;
+      }
     }
     const bool slow = MODE == FORWARD && odd_value && __any(sees != 0xffu);
+    // The forward pass sums a tile's products on their own before they join the row's: one chain of additions over thousands of keys
+    // loses a digit (float32, 1821 keys: 1.1e-6 of the result, so 4e-7).
+    f32x4 sum[NACC][NC][4];
+#pragma unroll
+    for (int x = 0; x < NACC; ++x)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) sum[x][c][ct] = MODE == FORWARD ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[x][c][ct];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -308,7 +325,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
           if (MODE == FORWARD) {
             if (!slow) {
 #pragma unroll
-              for (int ct = 0; ct < 4; ++ct) acc[0][c][ct] = mfma(a2[ct], p[kb][r], acc[0][c][ct]);
+              for (int ct = 0; ct < 4; ++ct) sum[0][c][ct] = mfma(a2[ct], p[kb][r], sum[0][c][ct]);
             } else {
               // one key at a time, added only to the rows that see it: zero times infinity stays out of the others
 #pragma unroll
@@ -318,26 +335,39 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
                 for (int ct = 0; ct < 4; ++ct) {
                   const f32x4 one = mfma(g == gg ? a2[ct] : 0.f, p[kb][r], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) acc[0][c][ct][e] += v ? one[e] : 0.f;
+                  for (int e = 0; e < 4; ++e) sum[0][c][ct][e] += v ? one[e] : 0.f;
                 }
               }
             }
           } else if (MODE == GRAD_Q) {
             const f32x4 a1 = *reinterpret_cast<const f32x4*>(&x1[row][64 * c + 4 * li]);
 #pragma unroll
-            for (int ct = 0; ct < 4; ++ct) acc[0][c][ct] = mfma(a1[ct], ds[kb][r], acc[0][c][ct]);
+            for (int ct = 0; ct < 4; ++ct) sum[0][c][ct] = mfma(a1[ct], ds[kb][r], sum[0][c][ct]);
           } else {
             const f32x4 a1 = *reinterpret_cast<const f32x4*>(&x1[row][64 * c + 4 * li]);
 #pragma unroll
             for (int ct = 0; ct < 4; ++ct) {
-              acc[0][c][ct] = mfma(a1[ct], ds[kb][r], acc[0][c][ct]);
-              acc[NACC - 1][c][ct] = mfma(a2[ct], p[kb][r], acc[NACC - 1][c][ct]);
+              sum[0][c][ct] = mfma(a1[ct], ds[kb][r], sum[0][c][ct]);
+              sum[NACC - 1][c][ct] = mfma(a2[ct], p[kb][r], sum[NACC - 1][c][ct]);
             }
           }
         }
       }
+#pragma unroll
+    for (int x = 0; x < NACC; ++x)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) acc[x][c][ct] = MODE == FORWARD ? acc[x][c][ct] * keep + sum[x][c][ct] : sum[x][c][ct];
     __syncthreads();
   }
+  if (MODE == GRAD_Q && round == 0) {
+    d_sum += __shfl_xor(d_sum, 16);
+    d_sum += __shfl_xor(d_sum, 32);
+    o_delta = d_sum;
+  }
+  }
+  if (MODE == GRAD_Q && ovalid && g == 0) P.delta[stat_of(orow)] = o_delta;
 
   // ---- epilogue -----------------------------------------------------------------------------------------------------------------
   float f = P.scale;
