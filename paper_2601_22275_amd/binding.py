@@ -144,7 +144,7 @@ def lib() -> ctypes.CDLL:
             getattr(L, "vmonarch_paged_attention" + suffix).argtypes = [c_void_p] * 4 + [c_int, n, c_int, c_int, c_int, c_float, c_int, c_void_p,
                                                                                         c_size_t, c_void_p]
         L.vmonarch_packed_attention_bwd_workspace_bytes.restype = c_size_t
-        L.vmonarch_packed_attention_bwd_workspace_bytes.argtypes = [n, c_int]
+        L.vmonarch_packed_attention_bwd_workspace_bytes.argtypes = [c_int, n, n, c_int, c_int, c_int]
         L.vmonarch_paged_attention_workspace_bytes.restype = c_size_t
         L.vmonarch_paged_attention_workspace_bytes.argtypes = [c_void_p, c_int, n, c_int, c_int, c_int]
         _lib = L
@@ -523,9 +523,10 @@ def packed_attention_bwd(q, k, v, out, d_out, lse, q_starts, k_starts=None, caus
         _same_shape(name, x, y)
     if lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous() or tuple(lse.shape) != (heads, nq):
         raise VMonarchError("lse: the log-sum-exp of packed_attention is needed, float32 [heads_q, tokens_q]")
-    if workspace is None:
-        workspace = torch.empty(lib().vmonarch_packed_attention_bwd_workspace_bytes(nq, heads), dtype=torch.uint8, device=q.device)
     n = q_starts.numel()
+    if workspace is None:
+        size = lib().vmonarch_packed_attention_bwd_workspace_bytes(n - 1, nq, k.shape[0], heads, k.shape[1], d)
+        workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
     x = [_tokens(name, t, q) for name, t in (("q", q), ("k", k), ("v", v), ("out", out), ("d_out", d_out), ("dq", dq), ("dk", dk), ("dv", dv))]
     p = [ctypes.byref(t) for t in x]
     size = workspace.numel() * workspace.element_size()

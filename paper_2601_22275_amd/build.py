@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libvmonarch.so")
 # (source, object, flags of its own): flash2.hip and seq_mfma.hip are compiled once per head dimension
 SOURCES = [(s, s.replace(".hip", ".o"), []) for s in ("api.hip", "generic.hip", "flash.hip", "flash_kv.hip", "frame.hip", "lpass.hip",
-                                                      "backward.hip", "backward_mfma.hip", "f32.hip", "rotary.hip", "seq_api.hip", "seq_general.hip")]
+                                                      "backward.hip", "backward_mfma.hip", "f32.hip", "rotary.hip", "seq_api.hip", "seq_general.hip", "seq_token.hip", "seq_bwd.hip")]
 SOURCES += [("flash2.hip", f"flash2_{d}.o", [f"-DVM_FLASH2_D={d}"]) for d in (64, 128)]
 SOURCES += [("seq_mfma.hip", f"seq_mfma_{d}.o", [f"-DVM_SEQ_D={d}"]) for d in (64, 128)]
 FLAGS = [
@@ -28,6 +28,8 @@ EXTRA = {"flash2.hip": ["-fno-honor-nans", "-Wno-inline-asm"],
          "frame.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-fno-honor-nans"],
          "f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
          "seq_mfma.hip": ["-fno-honor-nans", "-Wno-inline-asm"],
+         "seq_token.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+         "seq_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
          "seq_general.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
          "backward_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 

@@ -2,7 +2,6 @@
 #pragma once
 #include "../../include/vmonarch_sequence.h"
 #include "common.h"
-#include <stdlib.h>
 
 namespace vm {
 
@@ -47,7 +46,7 @@ struct SeqParams {
   // backward
   Rows<const E> o, d_out;
   Rows<E> dq, dk, dv;
-  float* delta;         // d_out . out per row, [heads_q][tokens_q]
+  float* delta;         // per row: seq_general.hip d_out . out, [heads_q][tokens_q]; seq_bwd.hip see there
   // ranges of keys (seq_paged.hip)
   float* part_o;
   float* part_s;
@@ -135,8 +134,18 @@ hipError_t launch_rotary(const RotaryParams& P, const RotaryTurns& F, int elem_b
 // seq_mfma.hip : bf16, aligned rows, d <= D (compiled for D = 64 and 128)
 template <int D>
 hipError_t launch_seq_attention_mfma(const SeqParams<bf16_t>& P, hipStream_t st);
-// Two 32-row query tiles per wave, or one
-inline bool seq_two_tiles(const SeqParams<bf16_t>& P) { return getenv("VM_TWO") ? atoi(getenv("VM_TWO")) : 0; }
+// seq_token.hip : the same for few rows (pages), and the join of ranges for everything that is cut into them
+template <int D>
+hipError_t launch_seq_token(const SeqParams<bf16_t>& P, hipStream_t st);
+template <typename E>
+hipError_t launch_seq_join(const SeqParams<E>& P, hipStream_t st);
+// Channels of a partial result's row
+inline int seq_padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+
+// seq_bwd.hip : the backward pass, bf16, aligned rows, d <= D (ranges: of query rows, for dK and dV; part_o their partial sums)
+int seq_bwd_ranges(int n_seqs, long long tokens_q, long long tokens_k, int heads_kv, int group);
+template <int D>
+hipError_t launch_seq_bwd_mfma(const SeqParams<bf16_t>& P, hipStream_t st);
 
 // seq_general.hip : any d <= 256, any strides, on the fp32 matrix units
 template <typename E>

@@ -40,9 +40,7 @@ int check_sizes(int n_seqs, long long tokens_q, long long tokens_k, int heads_q,
   if (d > 256) return api_fail(VMONARCH_ERR_UNSUPPORTED, "d=%d exceeds 256", d);
   if (heads_q > 65535) return api_fail(VMONARCH_ERR_UNSUPPORTED, "heads_q=%d exceeds 65535", heads_q);
   if (tokens_q > 0x7fffff00LL || tokens_k > 0x7fffff00LL) return api_fail(VMONARCH_ERR_UNSUPPORTED, "more than 2^31 - 256 tokens");
-  // one workgroup takes at least 32 packed rows, and a row of workgroups has fewer than 2^31 in x
-  if (tokens_q * (heads_q / heads_kv) / 32 + n_seqs > 0x7fffff00LL || tokens_k / 32 + n_seqs > 0x7fffff00LL)
-    return api_fail(VMONARCH_ERR_UNSUPPORTED, "more rows of queries or keys than one launch takes");
+  if (tokens_q * (heads_q / heads_kv) > 0x7fffff00LL) return api_fail(VMONARCH_ERR_UNSUPPORTED, "more rows of queries than one launch takes");
   return VMONARCH_OK;
 }
 
@@ -205,12 +203,46 @@ int append_impl(const vmonarch_tokens* k, const vmonarch_tokens* v, const vmonar
   return hip_result(launch_rotary(P, F, (int)elem, c.aligned && wide_pieces(P.interleaved, pairs, d, elem), as_stream(stream)), "paged_append launch");
 }
 
+// Pages: whether the rows go to the kernel for few of them, and into how many ranges the keys are cut
+struct PagedPlan {
+  bool few;
+  int ranges;
+};
+PagedPlan paged_plan(long long table_keys, int n_seqs, long long tokens, int heads_kv, int group) {
+  PagedPlan p;
+  const long long rows = tokens * group;
+  p.few = rows <= 32LL * n_seqs;
+  const long long blocks = tile_bound(tokens, group, p.few ? 32 : 128, n_seqs) * heads_kv;
+  const long long want = (p.few ? 4LL : 2LL) * compute_units();
+  const long long shortest = p.few ? 256 : 512;
+  long long r = (want + blocks - 1) / blocks;
+  if (r > (table_keys + shortest - 1) / shortest) r = (table_keys + shortest - 1) / shortest;
+  p.ranges = r > 64 ? 64 : (int)r;
+  return p;
+}
+
 template <typename E>
-hipError_t launch_attention(const SeqParams<E>& P, hipStream_t st) {
+hipError_t launch_attention(const SeqParams<E>& P, bool few, hipStream_t st) {
+  hipError_t e;
   if constexpr (sizeof(E) == 2) {
-    if (P.aligned && P.d <= 128) return P.d <= 64 ? launch_seq_attention_mfma<64>(P, st) : launch_seq_attention_mfma<128>(P, st);
+    if (P.aligned && P.d <= 128) {
+      if (few) e = P.d <= 64 ? launch_seq_token<64>(P, st) : launch_seq_token<128>(P, st);
+      else e = P.d <= 64 ? launch_seq_attention_mfma<64>(P, st) : launch_seq_attention_mfma<128>(P, st);
+    } else {
+      e = launch_seq_attention_general<E>(P, st);
+    }
+  } else {
+    e = launch_seq_attention_general<E>(P, st);
   }
-  return launch_seq_attention_general<E>(P, st);
+  return e == hipSuccess && P.ranges > 1 ? launch_seq_join<E>(P, st) : e;
+}
+
+template <typename E>
+hipError_t launch_attention_bwd(const SeqParams<E>& P, hipStream_t st) {
+  if constexpr (sizeof(E) == 2) {
+    if (P.aligned && P.d <= 128) return P.d <= 64 ? launch_seq_bwd_mfma<64>(P, st) : launch_seq_bwd_mfma<128>(P, st);
+  }
+  return launch_seq_attention_bwd_general<E>(P, st);
 }
 
 // ---- attention ------------------------------------------------------------------------------------------------------------------
@@ -239,7 +271,21 @@ int packed_impl(const vmonarch_tokens* q, const vmonarch_tokens* k, const vmonar
   P.heads_kv = heads_kv; P.group = heads_q / heads_kv; P.d = d;
   P.causal = causal != 0; P.scale = scale;
   P.aligned = c.aligned && d % (16 / (int)sizeof(E)) == 0;
-  return hip_result(launch_attention<E>(P, as_stream(stream)), "packed_attention launch");
+  return hip_result(launch_attention<E>(P, false, as_stream(stream)), "packed_attention launch");
+}
+
+// Workspace of the backward pass: two statistics per query row, then the partial dK and dV of the ranges of rows
+struct BwdLayout {
+  size_t parts, total;
+  int ranges;
+};
+BwdLayout bwd_layout(int n_seqs, long long tokens_q, long long tokens_k, int heads_q, int heads_kv, int d) {
+  BwdLayout l;
+  l.ranges = d <= 128 ? seq_bwd_ranges(n_seqs, tokens_q, tokens_k, heads_kv, heads_q / heads_kv) : 1;
+  l.parts = ((size_t)tokens_q * heads_q * 2 * sizeof(float) + 255) & ~(size_t)255;
+  l.total = l.parts;
+  if (l.ranges > 1) l.total += ((size_t)l.ranges * 2 * tokens_k * heads_kv * seq_padded(d) * sizeof(float) + 255) & ~(size_t)255;
+  return l;
 }
 
 template <typename E>
@@ -270,10 +316,14 @@ int packed_bwd_impl(const vmonarch_tokens* q, const vmonarch_tokens* k, const vm
     return api_fail(VMONARCH_ERR_INVALID_ARG, "workspace and workspace_bytes must both be zero or both non-zero");
   if (tokens_q == 0 && tokens_k == 0) return VMONARCH_OK;
   SeqParams<E> P = {};
-  const size_t need = vmonarch_packed_attention_bwd_workspace_bytes(tokens_q, heads_q);
-  if (need > 0) {
-    P.delta = (float*)api_workspace(need, &rc, workspace, workspace_bytes, as_stream(stream));
+  P.ranges = 1;
+  if (tokens_q > 0) {
+    const BwdLayout l = bwd_layout(n_seqs, tokens_q, tokens_k, heads_q, heads_kv, d);
+    char* ws = (char*)api_workspace(l.total, &rc, workspace, workspace_bytes, as_stream(stream));
     if (rc) return rc;
+    P.delta = (float*)ws;
+    P.part_o = (float*)(ws + l.parts);
+    P.ranges = l.ranges;
   }
   P.q = rows<const E>(q); P.k = key_rows<E>(k); P.v = key_rows<E>(v); P.o = rows<const E>(out); P.d_out = rows<const E>(d_out);
   P.dq = rows<E>(dq); P.dk = rows<E>(dk); P.dv = rows<E>(dv);
@@ -283,7 +333,7 @@ int packed_bwd_impl(const vmonarch_tokens* q, const vmonarch_tokens* k, const vm
   P.heads_kv = heads_kv; P.group = heads_q / heads_kv; P.d = d;
   P.causal = causal != 0; P.scale = scale;
   P.aligned = c.aligned && d % (16 / (int)sizeof(E)) == 0;
-  return hip_result(launch_seq_attention_bwd_general<E>(P, as_stream(stream)), "packed_attention_bwd launch");
+  return hip_result(launch_attention_bwd<E>(P, as_stream(stream)), "packed_attention_bwd launch");
 }
 
 template <typename E>
@@ -313,7 +363,15 @@ int paged_impl(const vmonarch_tokens* q, const vmonarch_cache* cache, const vmon
   P.heads_kv = heads_kv; P.group = heads_q / heads_kv; P.d = d;
   P.causal = causal != 0; P.scale = scale;
   P.aligned = c.aligned && d % (16 / (int)sizeof(E)) == 0;
-  return hip_result(launch_attention<E>(P, as_stream(stream)), "paged_attention launch");
+  const PagedPlan plan = paged_plan((long long)cache->table_width * cache->page_size, n_seqs, tokens, heads_kv, P.group);
+  P.ranges = plan.ranges;
+  if (plan.ranges > 1) {
+    const size_t need = vmonarch_paged_attention_workspace_bytes(cache, n_seqs, tokens, heads_q, heads_kv, d);
+    P.part_o = (float*)api_workspace(need, &rc, workspace, workspace_bytes, as_stream(stream));
+    if (rc) return rc;
+    P.part_s = P.part_o + (size_t)plan.ranges * tokens * heads_q * seq_padded(d);
+  }
+  return hip_result(launch_attention<E>(P, plan.few, as_stream(stream)), "paged_attention launch");
 }
 
 }  // namespace
@@ -379,9 +437,9 @@ int vmonarch_packed_attention_f32(const vmonarch_tokens* q, const vmonarch_token
   return packed_impl<float>(q, k, v, out, lse, q_starts, k_starts, n_seqs, tokens_q, tokens_k, heads_q, heads_kv, d, scale, causal, stream);
 }
 
-size_t vmonarch_packed_attention_bwd_workspace_bytes(long long tokens_q, int heads_q) {
-  if (tokens_q <= 0 || heads_q <= 0) return 0;
-  return ((size_t)tokens_q * heads_q * sizeof(float) + 255) & ~(size_t)255;
+size_t vmonarch_packed_attention_bwd_workspace_bytes(int n_seqs, long long tokens_q, long long tokens_k, int heads_q, int heads_kv, int d) {
+  if (n_seqs < 1 || tokens_q < 1 || tokens_k < 0 || heads_kv < 1 || heads_q < heads_kv || heads_q % heads_kv != 0 || d < 1 || d > 256) return 0;
+  return bwd_layout(n_seqs, tokens_q, tokens_k, heads_q, heads_kv, d).total;
 }
 int vmonarch_packed_attention_bwd(const vmonarch_tokens* q, const vmonarch_tokens* k, const vmonarch_tokens* v, const vmonarch_tokens* out,
                                   const vmonarch_tokens* d_out, const float* lse, const vmonarch_tokens* dq, const vmonarch_tokens* dk,
@@ -412,8 +470,12 @@ int vmonarch_paged_append_f32(const vmonarch_tokens* k, const vmonarch_tokens* v
 }
 
 size_t vmonarch_paged_attention_workspace_bytes(const vmonarch_cache* cache, int n_seqs, long long tokens, int heads_q, int heads_kv, int d) {
-  (void)cache; (void)n_seqs; (void)tokens; (void)heads_q; (void)heads_kv; (void)d;
-  return 0;
+  if (cache == nullptr || cache->table_width < 1 || cache->page_size < 1 || n_seqs < 1 || tokens < 1 || heads_kv < 1 || heads_q < heads_kv ||
+      heads_q % heads_kv != 0 || d < 1 || d > 256)
+    return 0;
+  const PagedPlan plan = paged_plan((long long)cache->table_width * cache->page_size, n_seqs, tokens, heads_kv, heads_q / heads_kv);
+  if (plan.ranges < 2) return 0;
+  return ((size_t)plan.ranges * tokens * heads_q * (seq_padded(d) + 1) * sizeof(float) + 255) & ~(size_t)255;
 }
 int vmonarch_paged_attention(const vmonarch_tokens* q, const vmonarch_cache* cache, const vmonarch_tokens* out, const int32_t* q_starts, int n_seqs,
                              long long tokens, int heads_q, int heads_kv, int d, float scale, int causal, void* workspace, size_t workspace_bytes,

@@ -162,6 +162,11 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
     const long long last = min(o0 + BM, owners) - 1;
     s1 = min(max((long long)more + 1 + last / group, 0LL), (long long)nk);
   }
+  if (MODE == FORWARD && P.ranges > 1) {  // this workgroup's range of keys
+    const long long per = ((nk + P.ranges - 1) / P.ranges + 63) & ~63;
+    s0 = min(blockIdx.z * per, s1);
+    s1 = min(s0 + per, s1);
+  }
   const int ntiles = (int)((s1 - s0 + BN - 1) / BN);
   constexpr int PIECES = BN * D / 4 / 256;  // 4-channel pieces of a tile per thread
   f32x4 f1[PIECES], f2[PIECES];
@@ -256,7 +261,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const bool v = base + 16 * kb + 4 * g + r < limit;
+          const bool v = base + 16 * kb + 4 * g + r < min((long long)limit, s1);
           sees |= (unsigned)v << (4 * kb + r);
           s[kb][r] = v ? s[kb][r] * sc : -INFINITY;
           top = fmaxf(top, s[kb][r]);
@@ -330,7 +335,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
               // one key at a time, added only to the rows that see it: zero times infinity stays out of the others
 #pragma unroll
               for (int gg = 0; gg < 4; ++gg) {
-                const bool v = base + 16 * kb + 4 * gg + r < limit;
+                const bool v = base + 16 * kb + 4 * gg + r < min((long long)limit, s1);
 #pragma unroll
                 for (int ct = 0; ct < 4; ++ct) {
                   const f32x4 one = mfma(g == gg ? a2[ct] : 0.f, p[kb][r], f32x4{0.f, 0.f, 0.f, 0.f});
@@ -377,6 +382,17 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
     f = l == 0.f ? 0.f : 1.0f / l;
   }
   if (!ovalid) return;
+  if (MODE == FORWARD && P.ranges > 1) {
+    const long long at = ((long long)blockIdx.z * P.heads_kv + kvh) * ((long long)P.tokens_q * group) + (long long)q_begin * group + orow;
+    if (g == 0) P.part_s[at] = l == 0.f ? -INFINITY : m + __log2f(l);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<f32x4*>(P.part_o + at * D + 64 * c + 16 * g + 4 * r) =
+            f32x4{acc[0][c][0][r] * f, acc[0][c][1][r] * f, acc[0][c][2][r] * f, acc[0][c][3][r] * f};
+    return;
+  }
   if (MODE == FORWARD && P.lse != nullptr && g == 0) P.lse[stat_of(orow)] = l == 0.f ? -INFINITY : LN2 * (m + __log2f(l));
   auto target = [&](const Rows<E>& X) -> E* {
     if (MODE == GRAD_KV) return X.p + (k_begin + orow) * X.t + kvh * X.h;
@@ -399,7 +415,7 @@ template <typename E, int MODE>
 hipError_t launch(const SeqParams<E>& P, hipStream_t st) {
   const long long tiles = MODE == GRAD_KV ? tile_bound(P.tokens_k, 1, BM, P.n_seqs) : tile_bound(P.tokens_q, P.group, BM, P.n_seqs);
   if (tiles > 0x7fffffffLL) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)tiles, (unsigned)P.heads_kv);
+  const dim3 grid((unsigned)tiles, (unsigned)P.heads_kv, (unsigned)(MODE == FORWARD && P.ranges > 1 ? P.ranges : 1));
   if (P.d <= 64) hipLaunchKernelGGL((seq_general_kernel<E, 64, MODE>), grid, dim3(256), 0, st, P);
   else if (P.d <= 128) hipLaunchKernelGGL((seq_general_kernel<E, 128, MODE>), grid, dim3(256), 0, st, P);
   else hipLaunchKernelGGL((seq_general_kernel<E, 256, MODE>), grid, dim3(256), 0, st, P);

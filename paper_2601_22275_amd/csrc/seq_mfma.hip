@@ -1,6 +1,6 @@
 // bf16 attention over packed sequences and over pages on gfx950: d <= 128, a multiple of 8 (padded to 64 or 128 channels in LDS).
 //
-// One workgroup = 4 waves of one or two 32-row query tiles; query rows are packed (token, head of the group), so that the heads that share
+// One workgroup = 4 waves of 32 query rows, two workgroups on a compute unit; query rows are packed (token, head of the group), so that the heads that share
 // keys share a tile and its LDS reads.  Keys and values stream through LDS in tiles (four slots per tensor, loaded two tiles ahead straight
 // from memory, chunks swizzled as RowGeo says), and both products are v_mfma_f32_32x32x16_bf16 on transposed operands:
 //   S^T = K Q^T        lane (q, g) holds the logits of query q for 16 of 32 keys: sums of a row are per-lane scalars
@@ -13,7 +13,9 @@
 // products of n - 1 dealt over the same instruction slots); the tiles at the end of the range that some row sees in part or
 // not at all (the diagonal, the ragged end) follow in plain order, with a true running maximum, masks, and a look at the values: zero times
 // infinity must not reach a row that does not see the key.
-// Bound by the matrix units, which at one 32-row tile a wave share the LDS with the operand reads.
+// Bound by the matrix units and the LDS that feeds them (an operand per MFMA).  Two 32-row tiles per wave, which halve those reads and
+// leave one wave on a SIMD, measured level at 16,384 tokens (885 against 861 TFLOP/s at d = 128, 699 against 793 at d = 64) and behind on
+// everything shorter (16 x 1000 tokens, 12 heads, d = 128: 97 us against 68).
 #include <type_traits>
 
 #include "seq_device.h"
@@ -36,20 +38,20 @@ constexpr float MOVE_ALONG2 = 8.0f;   // rows of the wave this far above their r
 #define SQ_MFMA_RESULT_WAIT() asm volatile("s_nop 15\n\ts_nop 3" ::: "memory")
 
 // Key rows of an LDS tile: two workgroups share a compute unit at 32 rows and d = 128
-template <int D, int Q2>
+template <int D>
 constexpr int tile_rows() {
-  return D == 128 && Q2 == 1 ? 32 : 64;
+  return D == 128 ? 32 : 64;
 }
 
-template <int D, bool PAGED, bool SPLIT, bool STAT, int Q2>
-__global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel(SeqParams<bf16_t> P) {
+template <int D, bool PAGED, bool SPLIT, bool STAT>
+__global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf16_t> P) {
   using G = RowGeo<D>;
   constexpr int ROW_BYTES = G::ROW_BYTES;
-  constexpr int BT = tile_rows<D, Q2>();
+  constexpr int BT = tile_rows<D>();
   constexpr int TILE_BYTES = BT * ROW_BYTES;
   constexpr int KS = G::KS, CT = G::CT, CH = G::CH, RPI = G::RPI;
   constexpr int V_OFF = NSLOT * TILE_BYTES;
-  constexpr int BQ = 32 * Q2 * W2;
+  constexpr int BQ = 32 * W2;
   auto swz = [](int row) { return G::swz(row); };
   extern __shared__ __attribute__((aligned(16))) char smem[];  // [K|V][NSLOT][BT rows][2 D bytes]
 
@@ -157,19 +159,16 @@ __global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel
 
   // ---- queries: B operand of S^T = K Q^T ------------------------------------------------------------------------------------------
   // Packed row r as (token, head), clamped to the last row; and how many keys of this range it sees
-  bf16x8 qreg[Q2][KS];
-  int limit[Q2];
+  bf16x8 qreg[KS];
+  int limit;
   const float sc = P.scale * LOG2E;
+  const long long r = min(row_first + wave * 32 + ql, rows - 1);
+  const int tok = (int)(r / group);
+  const bf16_t* qp = P.q.p + (long long)(w.begin + tok) * P.q.t + (kvh * group + (int)(r - (long long)tok * group)) * P.q.h + 8 * g;
+  const bf16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-  for (int qt = 0; qt < Q2; ++qt) {
-    const long long r = min(row_first + wave * (32 * Q2) + qt * 32 + ql, rows - 1);
-    const int tok = (int)(r / group);
-    const bf16_t* qp = P.q.p + (long long)(w.begin + tok) * P.q.t + (kvh * group + (int)(r - (long long)tok * group)) * P.q.h + 8 * g;
-    const bf16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qreg[qt][ks] = 16 * ks + 8 * g < P.d ? *reinterpret_cast<const bf16x8*>(qp + 16 * ks) : zero;
-    limit[qt] = (P.causal ? (int)min(max(more + 1 + tok, 0LL), (long long)nk) : nk) - k0;
-  }
+  for (int ks = 0; ks < KS; ++ks) qreg[ks] = 16 * ks + 8 * g < P.d ? *reinterpret_cast<const bf16x8*>(qp + 16 * ks) : zero;
+  limit = (P.causal ? (int)min(max(more + 1 + tok, 0LL), (long long)nk) : nk) - k0;
 
   // ---- LDS read addresses (see RowGeo): everything but these is an instruction immediate --------------------------------------------
   unsigned a_off[KS];
@@ -216,25 +215,19 @@ __global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
   };
 
-  f32x16 oacc[Q2][CT];
-#pragma unroll
-  for (int qt = 0; qt < Q2; ++qt)
+  f32x16 oacc[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) oacc[qt][ct][r] = 0.f;
-  float msc[Q2], ltil[Q2], lsum[Q2];  // reference, sum of the rounded weights, of the unrounded ones
-#pragma unroll
-  for (int qt = 0; qt < Q2; ++qt) {
-    msc[qt] = NEG_BIG;
-    ltil[qt] = 0.f;
-    lsum[qt] = 0.f;
-  }
+      for (int r = 0; r < 16; ++r) oacc[ct][r] = 0.f;
+  float msc, ltil, lsum;  // reference, sum of the rounded weights, of the unrounded ones
+  msc = NEG_BIG;
+  ltil = 0.f;
+  lsum = 0.f;
 
-  // ---- one step of the pipeline (see the top): KS groups of logits, then 2 CT groups of products, one MFMA per query tile each --------
+  // ---- one step of the pipeline (see the top): KS groups of logits, then 2 CT groups of products --------
   constexpr int NPV = 2 * CT;
   constexpr int NG = KS + NPV;
-  constexpr int NSL = Q2 * NG;
   constexpr int PF = 2, RING = 4;
   static_assert(NG % RING == 0 && RING > PF, "ring positions repeat from step to step");
   bf16x8 ring[RING];
@@ -247,12 +240,11 @@ __global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel
       ring[GI % RING] = rd_value(ct, pv_off + c * 16 * ROW_BYTES);
     }
   };
-  auto issue = [&](auto gc, auto qc, f32x16 (&snext)[Q2], bf16x8 (&pbprev)[Q2][2]) __attribute__((always_inline)) {
+  auto issue = [&](auto gc, f32x16 &snext, bf16x8 (&pbprev)[2]) __attribute__((always_inline)) {
     constexpr int GI = decltype(gc)::value;
-    constexpr int qt = decltype(qc)::value;
-    if constexpr (GI == 0) mfma_first(snext[qt], ring[GI % RING], qreg[qt][GI]);
-    else if constexpr (GI < KS) mfma_v(snext[qt], ring[GI % RING], qreg[qt][GI]);
-    else mfma_a(oacc[qt][(GI - KS) % CT], ring[GI % RING], pbprev[qt][(GI - KS) / CT]);
+    if constexpr (GI == 0) mfma_first(snext, ring[GI % RING], qreg[GI]);
+    else if constexpr (GI < KS) mfma_v(snext, ring[GI % RING], qreg[GI]);
+    else mfma_a(oacc[(GI - KS) % CT], ring[GI % RING], pbprev[(GI - KS) / CT]);
   };
 
   typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
@@ -261,44 +253,41 @@ __global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel
   ones2[1] = (__bf16)1.0f;
   // Two scores of one query tile in three stages, each in an MFMA slot of its own
   float tq[2][2], pq[2][2];
-  float ltstep[Q2], lstep[Q2];
-  auto score_scale = [&](auto kc, f32x16 (&scur)[Q2]) __attribute__((always_inline)) {
-    constexpr int K = decltype(kc)::value, qt = K % Q2, j = K / Q2;
-    tq[K & 1][0] = __builtin_fmaf(scur[qt][2 * j], sc, -msc[qt]);
-    tq[K & 1][1] = __builtin_fmaf(scur[qt][2 * j + 1], sc, -msc[qt]);
+  float ltstep, lstep;
+  auto score_scale = [&](auto kc, f32x16 &scur) __attribute__((always_inline)) {
+    constexpr int K = decltype(kc)::value, j = K;
+    tq[K & 1][0] = __builtin_fmaf(scur[2 * j], sc, -msc);
+    tq[K & 1][1] = __builtin_fmaf(scur[2 * j + 1], sc, -msc);
   };
   auto score_exp = [&](auto kc) __attribute__((always_inline)) {
     constexpr int K = decltype(kc)::value;
     pq[K & 1][0] = __builtin_amdgcn_exp2f(tq[K & 1][0]);
     pq[K & 1][1] = __builtin_amdgcn_exp2f(tq[K & 1][1]);
   };
-  auto score_sums = [&](auto kc, bf16x8 (&pbcur)[Q2][2]) __attribute__((always_inline)) {
-    constexpr int K = decltype(kc)::value, qt = K % Q2, j = K / Q2;
+  auto score_sums = [&](auto kc, bf16x8 (&pbcur)[2]) __attribute__((always_inline)) {
+    constexpr int K = decltype(kc)::value, j = K;
     bf16x2 pr;
     pr[0] = (__bf16)pq[K & 1][0];
     pr[1] = (__bf16)pq[K & 1][1];
-    if (STAT) lstep[qt] = (j == 0 ? pq[K & 1][0] : lstep[qt] + pq[K & 1][0]) + pq[K & 1][1];
-    ltstep[qt] = __builtin_amdgcn_fdot2_f32_bf16(pr, ones2, j == 0 ? 0.f : ltstep[qt], false);
-    pbcur[qt][j >> 2][2 * (j & 3)] = pr[0];
-    pbcur[qt][j >> 2][2 * (j & 3) + 1] = pr[1];
-    asm volatile("" : "+v"(ltstep[qt]));
-    if (STAT) asm volatile("" : "+v"(lstep[qt]));
+    if (STAT) lstep = (j == 0 ? pq[K & 1][0] : lstep + pq[K & 1][0]) + pq[K & 1][1];
+    ltstep = __builtin_amdgcn_fdot2_f32_bf16(pr, ones2, j == 0 ? 0.f : ltstep, false);
+    pbcur[j >> 2][2 * (j & 3)] = pr[0];
+    pbcur[j >> 2][2 * (j & 3) + 1] = pr[1];
+    asm volatile("" : "+v"(ltstep));
+    if (STAT) asm volatile("" : "+v"(lstep));
   };
-  auto plain_logits = [&](int off, f32x16 (&s)[Q2]) __attribute__((always_inline)) {
+  auto plain_logits = [&](int off, f32x16 &s) __attribute__((always_inline)) {
     static_for<0, KS>([&](auto kc) {
       constexpr int ks = decltype(kc)::value;
       const bf16x8 a = rd_row(kc, off);
-#pragma unroll
-      for (int qt = 0; qt < Q2; ++qt) {
-        if constexpr (ks == 0) mfma_first(s[qt], a, qreg[qt][ks]);
-        else mfma_v(s[qt], a, qreg[qt][ks]);
-      }
+      if constexpr (ks == 0) mfma_first(s, a, qreg[ks]);
+      else mfma_v(s, a, qreg[ks]);
     });
     SQ_MFMA_RESULT_WAIT();
     SQ_FENCE();
   };
-  auto plain_weights = [&](f32x16 (&s)[Q2], bf16x8 (&pb)[Q2][2]) __attribute__((always_inline)) {
-    static_for<0, 8 * Q2>([&](auto kc) {
+  auto plain_weights = [&](f32x16 &s, bf16x8 (&pb)[2]) __attribute__((always_inline)) {
+    static_for<0, 8>([&](auto kc) {
       score_scale(kc, s);
       score_exp(kc);
       score_sums(kc, pb);
@@ -306,14 +295,13 @@ __global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel
     asm volatile("s_nop 1" ::: "memory");
     SQ_FENCE();
   };
-  auto plain_products = [&](int off, bf16x8 (&pb)[Q2][2]) __attribute__((always_inline)) {
+  auto plain_products = [&](int off, bf16x8 (&pb)[2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
         const bf16x8 a = rd_value(ct, off + c * 16 * ROW_BYTES);
-#pragma unroll
-        for (int qt = 0; qt < Q2; ++qt) mfma_a(oacc[qt][ct], a, pb[qt][c]);
+        mfma_a(oacc[ct], a, pb[c]);
       }
   };
   // Products issued so far have reached the accumulators, and nothing reads those before this line
@@ -321,38 +309,33 @@ __global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel
     SQ_FENCE();
     SQ_MFMA_RESULT_WAIT();
 #pragma unroll
-    for (int qt = 0; qt < Q2; ++qt)
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) asm volatile("" : "+a"(oacc[qt][ct]));
+      for (int ct = 0; ct < CT; ++ct) asm volatile("" : "+a"(oacc[ct]));
     SQ_FENCE();
   };
-  // Rows of query tile qt whose maximum `cand` has outgrown the reference take one `headroom` above it; what they have is rescaled
-  auto move_reference = [&](int qt, float cand, float headroom) __attribute__((always_inline)) {
-    const float m = cand > msc[qt] + MOVE_ALONG2 ? cand + headroom : msc[qt];
-    const float alpha = __builtin_amdgcn_exp2f(msc[qt] - m);
-    lsum[qt] *= alpha;
-    ltil[qt] *= alpha;
-    msc[qt] = m;
+  // Rows whose maximum `cand` has outgrown the reference take one `headroom` above it; what they have is rescaled
+  auto move_reference = [&](float cand, float headroom) __attribute__((always_inline)) {
+    const float m = cand > msc + MOVE_ALONG2 ? cand + headroom : msc;
+    const float alpha = __builtin_amdgcn_exp2f(msc - m);
+    lsum *= alpha;
+    ltil *= alpha;
+    msc = m;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
       // one tile at a time, so that the copies out of the accumulation registers do not pile up
-      asm volatile("" : "+a"(oacc[qt][ct]));
+      asm volatile("" : "+a"(oacc[ct]));
 #pragma unroll
-      for (int r = 0; r < 16; ++r) oacc[qt][ct][r] *= alpha;
-      asm volatile("" : "+a"(oacc[qt][ct]));
+      for (int r = 0; r < 16; ++r) oacc[ct][r] *= alpha;
+      asm volatile("" : "+a"(oacc[ct]));
       SQ_FENCE();
     }
   };
   auto add_sums = [&]() __attribute__((always_inline)) {
-#pragma unroll
-    for (int qt = 0; qt < Q2; ++qt) {
-      ltil[qt] += ltstep[qt];
-      if (STAT) lsum[qt] += lstep[qt];
-    }
+    ltil += ltstep;
+    if (STAT) lsum += lstep;
   };
   // S_OFF / PV_OFF: byte offsets (slot and sub-tile) of this step's logits and products; NS_OFF / NPV_OFF: of the next step's
-  auto step = [&](auto s_c, auto pv_c, auto ns_c, auto npv_c, f32x16 (&scur)[Q2], f32x16 (&snext)[Q2], bf16x8 (&pbprev)[Q2][2],
-                  bf16x8 (&pbcur)[Q2][2]) __attribute__((always_inline)) {
+  auto step = [&](auto s_c, auto pv_c, auto ns_c, auto npv_c, f32x16 &scur, f32x16 &snext, bf16x8 (&pbprev)[2],
+                  bf16x8 (&pbcur)[2]) __attribute__((always_inline)) {
     constexpr int S_OFF = decltype(s_c)::value, PV_OFF = decltype(pv_c)::value;
     constexpr int NS_OFF = decltype(ns_c)::value, NPV_OFF = decltype(npv_c)::value;
     SQ_FENCE();
@@ -361,35 +344,30 @@ __global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel
       constexpr int GI = decltype(gc)::value;
       if constexpr (GI + PF < NG) request(std::integral_constant<int, GI + PF>{}, S_OFF, PV_OFF);
       else if constexpr (BT == 64) request(std::integral_constant<int, GI + PF - NG>{}, NS_OFF, NPV_OFF);
-      static_for<0, Q2>([&](auto qc) {
-        constexpr int SL = Q2 * GI + decltype(qc)::value;
-        issue(gc, qc, snext, pbprev);
-        static_for<0, 8 * Q2>([&](auto kc) {
-          constexpr int K = decltype(kc)::value;
-          constexpr int S0 = (K * NSL) / (8 * Q2);
-          constexpr int S1 = S0 + 1 < NSL ? S0 + 1 : NSL - 1;
-          constexpr int S2 = S0 + 2 < NSL ? S0 + 2 : NSL - 1;
-          if constexpr (S0 == SL) score_scale(kc, scur);
-          if constexpr (S1 == SL) score_exp(kc);
-          if constexpr (S2 == SL) score_sums(kc, pbcur);
-        });
-        SQ_FENCE();
+      issue(gc, snext, pbprev);
+      static_for<0, 8>([&](auto kc) {
+        constexpr int K = decltype(kc)::value;
+        constexpr int S0 = K * NG / 8;
+        constexpr int S1 = S0 + 1 < NG ? S0 + 1 : NG - 1;
+        constexpr int S2 = S0 + 2 < NG ? S0 + 2 : NG - 1;
+        if constexpr (S0 == GI) score_scale(kc, scur);
+        if constexpr (S1 == GI) score_exp(kc);
+        if constexpr (S2 == GI) score_sums(kc, pbcur);
       });
+      SQ_FENCE();
     });
-#pragma unroll
-    for (int qt = 0; qt < Q2; ++qt) asm volatile("" : "+v"(pbcur[qt][0]), "+v"(pbcur[qt][1]));
-    if (__any(ltstep[0] > STEP_LARGE2 || ltstep[Q2 - 1] > STEP_LARGE2)) {
+    asm volatile("" : "+v"(pbcur[0]), "+v"(pbcur[1]));
+    if (__any(ltstep > STEP_LARGE2)) {
       // the sub-tile just finished (its products are not issued yet) is formed again against new references
-      f32x16 s[Q2];
+      f32x16 s;
       plain_logits(NPV_OFF, s);
-#pragma unroll
-      for (int qt = 0; qt < Q2; ++qt) move_reference(qt, subtile_max(s[qt]) * sc, HEADROOM2);
+      move_reference(subtile_max(s) * sc, HEADROOM2);
       plain_logits(NPV_OFF, s);  // again: kept meanwhile they would sit beside the copies of the accumulators
       plain_weights(s, pbcur);
     }
     add_sums();
   };
-  const bool active = row_first + wave * (32 * Q2) < rows;  // a wave of padding only helps to load
+  const bool active = row_first + wave * 32 < rows;  // a wave of padding only helps to load
 
   int t = 0;  // tiles done
   auto next_tile = [&](int tt) __attribute__((always_inline)) {
@@ -406,17 +384,14 @@ __global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel
   if (nfull > 0) {
     // Tile t in slot t & 3: during tile t the products of tile t - 1's last sub-tile are outstanding, tile t + 1 is resident (its first
     // logits are needed a step ahead; behind the last whole tile they are of what comes there, and dropped), t + 2 in flight.
-    f32x16 sA[Q2], sB[Q2];
-    bf16x8 pbA[Q2][2], pbB[Q2][2];
+    f32x16 sA, sB;
+    bf16x8 pbA[2], pbB[2];
     const bf16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-    for (int qt = 0; qt < Q2; ++qt)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) pbB[qt][c] = zero;
+      for (int c = 0; c < 2; ++c) pbB[c] = zero;
     if (active) {
       plain_logits(0, sA);
-#pragma unroll
-      for (int qt = 0; qt < Q2; ++qt) msc[qt] = fmaxf(subtile_max(sA[qt]) * sc, NEG_BIG);
+      msc = fmaxf(subtile_max(sA) * sc, NEG_BIG);
       if constexpr (BT == 64) static_for<0, PF>([&](auto gc) { request(gc, 32 * ROW_BYTES, 3 * TILE_BYTES + 32 * ROW_BYTES); });
     }
     auto tile_iteration = [&](auto slot_c, int tt) __attribute__((always_inline)) {
@@ -447,11 +422,8 @@ __global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel
     if (active) {
       // the products of the last sub-tile; with one sub-tile per tile its weights' set goes by the slot
       if (BT == 32 && (nfull & 1)) {
-#pragma unroll
-        for (int qt = 0; qt < Q2; ++qt) {
-          pbB[qt][0] = pbA[qt][0];
-          pbB[qt][1] = pbA[qt][1];
-        }
+        pbB[0] = pbA[0];
+        pbB[1] = pbA[1];
         asm volatile("s_nop 1" ::: "memory");
       }
       plain_products(((nfull - 1) & 3) * TILE_BYTES + (BT - 32) * ROW_BYTES, pbB);
@@ -468,22 +440,18 @@ __global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel
       const int off = (t & 3) * TILE_BYTES + sub * 32 * ROW_BYTES;
       const int first = t * BT + 32 * sub;
       if (first >= nkeys) break;
-      f32x16 s[Q2];
-      bf16x8 pb[Q2][2];
+      f32x16 s;
+      bf16x8 pb[2];
       plain_logits(off, s);
       bool move = false;
-      float top[Q2];
+      float top;
+      const int left = min(limit, nkeys) - first - 4 * g;
 #pragma unroll
-      for (int qt = 0; qt < Q2; ++qt) {
-        const int left = min(limit[qt], nkeys) - first - 4 * g;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[qt][r] = 8 * (r >> 2) + (r & 3) < left ? s[qt][r] : -INFINITY;
-        top[qt] = subtile_max(s[qt]) * sc;
-        move = move || top[qt] > msc[qt] + MOVE_ALONG2;
-      }
+      for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < left ? s[r] : -INFINITY;
+      top = subtile_max(s) * sc;
+      move = move || top > msc + MOVE_ALONG2;
       if (__any(move)) {
-#pragma unroll
-        for (int qt = 0; qt < Q2; ++qt) move_reference(qt, top[qt], 0.f);
+        move_reference(top, 0.f);
       }
       plain_weights(s, pb);
       add_sums();
@@ -507,20 +475,17 @@ __global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel
 #pragma unroll
             for (int x = 0; x < 4; ++x) a32[x] &= x == e >> 1 ? part : 0u;
             __builtin_memcpy(&a, a32, 16);
+            const bool v = first + 16 * c + i < min(limit, nkeys);
+            f32x16 one;
+            asm volatile("s_nop 4");
+            mfma_first(one, a, pb[c]);
+            SQ_MFMA_RESULT_WAIT();
+            SQ_FENCE();
+            asm volatile("" : "+a"(oacc[ct]));
 #pragma unroll
-            for (int qt = 0; qt < Q2; ++qt) {
-              const bool v = first + 16 * c + i < min(limit[qt], nkeys);
-              f32x16 one;
-              asm volatile("s_nop 4");
-              mfma_first(one, a, pb[qt][c]);
-              SQ_MFMA_RESULT_WAIT();
-              SQ_FENCE();
-              asm volatile("" : "+a"(oacc[qt][ct]));
-#pragma unroll
-              for (int r = 0; r < 16; ++r) oacc[qt][ct][r] += v ? one[r] : 0.f;
-              asm volatile("" : "+a"(oacc[qt][ct]));
-              SQ_FENCE();
-            }
+            for (int r = 0; r < 16; ++r) oacc[ct][r] += v ? one[r] : 0.f;
+            asm volatile("" : "+a"(oacc[ct]));
+            SQ_FENCE();
           }
         }
     }
@@ -530,52 +495,49 @@ __global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel
   int tid_e = threadIdx.x;
   asm volatile("" : "+v"(tid_e));
   const int lane_e = tid_e & 63, ql_e = lane_e & 31, g_e = lane_e >> 5;
-  const long long wave_first = row_first + wave * (32 * Q2);
-  char* stage = smem + wave * (32 * Q2 * ROW_BYTES);
-  static_assert(W2 * 32 * Q2 * ROW_BYTES <= 2 * V_OFF, "staged rows fit the slots");
+  const long long wave_first = row_first + wave * 32;
+  char* stage = smem + wave * (32 * ROW_BYTES);
+  static_assert(W2 * 32 * ROW_BYTES <= 2 * V_OFF, "staged rows fit the slots");
+  SQ_FENCE();
+  const long long orow = wave_first + ql_e;
+  const float lt = ltil + __shfl_xor(ltil, 32);
+  const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+  if (SPLIT) {
+    if (orow < rows) {
+      // partial result of this range: [range][key head][packed row of all sequences]
+      const long long at = ((long long)blockIdx.y * P.heads_kv + kvh) * ((long long)P.tokens_q * group) + (long long)w.begin * group + orow;
+      if (g_e == 0) P.part_s[at] = lt == 0.f ? -INFINITY : msc + __log2f(lt);
 #pragma unroll
-  for (int qt = 0; qt < Q2; ++qt) {
-    SQ_FENCE();
-    const long long r = wave_first + qt * 32 + ql_e;
-    const float lt = ltil[qt] + __shfl_xor(ltil[qt], 32);
-    const float inv = lt == 0.f ? 0.f : 1.0f / lt;
-    if (SPLIT) {
-      if (r < rows) {
-        // partial result of this range: [range][key head][packed row of all sequences]
-        const long long at = ((long long)blockIdx.y * P.heads_kv + kvh) * ((long long)P.tokens_q * group) + (long long)w.begin * group + r;
-        if (g_e == 0) P.part_s[at] = lt == 0.f ? -INFINITY : msc[qt] + __log2f(lt);
+      for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const f32x4 x = {oacc[qt][ct][4 * c + 0] * inv, oacc[qt][ct][4 * c + 1] * inv, oacc[qt][ct][4 * c + 2] * inv, oacc[qt][ct][4 * c + 3] * inv};
-            *reinterpret_cast<f32x4*>(P.part_o + at * D + 32 * ct + 8 * c + 4 * g_e) = x;
-          }
-      }
-      continue;
+        for (int c = 0; c < 4; ++c) {
+          const f32x4 x = {oacc[ct][4 * c + 0] * inv, oacc[ct][4 * c + 1] * inv, oacc[ct][4 * c + 2] * inv, oacc[ct][4 * c + 3] * inv};
+          *reinterpret_cast<f32x4*>(P.part_o + at * D + 32 * ct + 8 * c + 4 * g_e) = x;
+        }
     }
-    if (STAT) {
-      const float l = lsum[qt] + __shfl_xor(lsum[qt], 32);
-      if (r < rows && g_e == 0) {
-        const int tok = (int)(r / group);
-        P.lse[(long long)(kvh * group + (int)(r - (long long)tok * group)) * P.tokens_q + w.begin + tok] = l == 0.f ? -INFINITY : LN2 * (msc[qt] + __log2f(l));
-      }
-    }
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint2 x;
-        x.x = pack_bf16(oacc[qt][ct][4 * c + 0] * inv, oacc[qt][ct][4 * c + 1] * inv);
-        x.y = pack_bf16(oacc[qt][ct][4 * c + 2] * inv, oacc[qt][ct][4 * c + 3] * inv);
-        *reinterpret_cast<uint2*>(stage + (32 * qt + ql_e) * ROW_BYTES + (((4 * ct + c) ^ swz(ql_e)) << 4) + 8 * g_e) = x;
-      }
+    return;
   }
+  if (STAT) {
+    const float l = lsum + __shfl_xor(lsum, 32);
+    if (orow < rows && g_e == 0) {
+      const int tok = (int)(orow / group);
+      P.lse[(long long)(kvh * group + (int)(orow - (long long)tok * group)) * P.tokens_q + w.begin + tok] = l == 0.f ? -INFINITY : LN2 * (msc + __log2f(l));
+    }
+  }
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      uint2 x;
+      x.x = pack_bf16(oacc[ct][4 * c + 0] * inv, oacc[ct][4 * c + 1] * inv);
+      x.y = pack_bf16(oacc[ct][4 * c + 2] * inv, oacc[ct][4 * c + 3] * inv);
+      *reinterpret_cast<uint2*>(stage + ql_e * ROW_BYTES + (((4 * ct + c) ^ swz(ql_e)) << 4) + 8 * g_e) = x;
+    }
   if (!SPLIT) {
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the staged rows are private to the wave
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int ps = 0; ps < 32 * Q2 / RPI; ++ps) {
+    for (int ps = 0; ps < 32 / RPI; ++ps) {
       const int lr = ps * RPI + lane_e / CH;
       const int pc = lane_e % CH;
       const int lc = pc ^ swz(lr);
@@ -589,12 +551,12 @@ __global__ void __launch_bounds__(64 * W2, Q2 == 1 ? 2 : 1) seq_attention_kernel
   }
 }
 
-template <int D, bool PAGED, bool SPLIT, bool STAT, int Q2>
+template <int D, bool PAGED, bool SPLIT, bool STAT>
 hipError_t launch(const SeqParams<bf16_t>& P, hipStream_t st) {
-  constexpr int LDS = 2 * NSLOT * tile_rows<D, Q2>() * D * 2;
-  const long long blocks = tile_bound(P.tokens_q, P.group, 32 * Q2 * W2, P.n_seqs) * P.heads_kv;
+  constexpr int LDS = 2 * NSLOT * tile_rows<D>() * D * 2;
+  const long long blocks = tile_bound(P.tokens_q, P.group, 32 * W2, P.n_seqs) * P.heads_kv;
   if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-  auto kern = seq_attention_kernel<D, PAGED, SPLIT, STAT, Q2>;
+  auto kern = seq_attention_kernel<D, PAGED, SPLIT, STAT>;
   static const hipError_t configured = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (configured != hipSuccess) return configured;
   hipLaunchKernelGGL(kern, dim3((unsigned)blocks, (unsigned)(SPLIT ? P.ranges : 1)), dim3(64 * W2), LDS, st, P);
@@ -608,13 +570,8 @@ hipError_t launch(const SeqParams<bf16_t>& P, hipStream_t st) {
 
 template <int D>
 hipError_t launch_seq_attention_mfma(const SeqParams<bf16_t>& P, hipStream_t st) {
-  const bool two = seq_two_tiles(P);
-  if (P.page_size > 0) {
-    if (P.ranges > 1) return launch<D, true, true, false, 1>(P, st);
-    return two ? launch<D, true, false, false, 2>(P, st) : launch<D, true, false, false, 1>(P, st);
-  }
-  if (P.lse != nullptr) return two ? launch<D, false, false, true, 2>(P, st) : launch<D, false, false, true, 1>(P, st);
-  return two ? launch<D, false, false, false, 2>(P, st) : launch<D, false, false, false, 1>(P, st);
+  if (P.page_size > 0) return P.ranges > 1 ? launch<D, true, true, false>(P, st) : launch<D, true, false, false>(P, st);
+  return P.lse != nullptr ? launch<D, false, false, true>(P, st) : launch<D, false, false, false>(P, st);
 }
 
 // This file is compiled once per head dimension.

@@ -62,8 +62,10 @@ def test_packed_attention_bwd_refusals():
     refuses(INVALID, go(ws=ctypes.c_void_p(100), size=4096), "256-byte")
     refuses(-3, go(ws=ctypes.c_void_p(256), size=16), "needed")
     refuses(INVALID, go(dv=T(1 << 20, 64, 0)), "stride of zero")
-    assert lib.vmonarch_packed_attention_bwd_workspace_bytes(0, 4) == 0
-    assert lib.vmonarch_packed_attention_bwd_workspace_bytes(10, 4) >= 160
+    size = lib.vmonarch_packed_attention_bwd_workspace_bytes
+    assert size(1, 0, 8, 4, 2, 64) == 0 and size(1, 8, 8, 4, 3, 64) == 0 and size(0, 8, 8, 4, 2, 64) == 0
+    assert size(1, 10, 8, 4, 2, 64) >= 320                       # two statistics per row
+    assert size(1, 100000, 128, 4, 2, 64) > 2 * 100000 * 4 * 4   # and partial sums where rows are many and keys few
 
 
 def cache(**kw):
