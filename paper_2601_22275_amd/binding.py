@@ -12,7 +12,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
-from ctypes import c_char_p, c_float, c_int, c_size_t, c_void_p
+from ctypes import byref, c_char_p, c_float, c_int, c_size_t, c_void_p
 
 import torch
 
@@ -419,27 +419,27 @@ def permute_tokens(x, T, Hs, Ws, to_position_major=True, out=None):
 
 
 def _sizes(name, x):
-    if x.dim() != 3:
-        raise VMonarchError(f"{name}: expected [tokens, heads, d], got {tuple(x.shape)}")
-    return x.shape
+    shape = x.shape
+    if len(shape) != 3:
+        raise VMonarchError(f"{name}: expected [tokens, heads, d], got {tuple(shape)}")
+    if not x.is_cuda:
+        raise VMonarchError(f"{name}: a CUDA tensor is needed")
+    return shape
 
 
-def _tokens(name, x, like=None):
+def _tokens(name, x, like):
     """The descriptor of token tensor x, checked against the type, device and head size of `like`."""
-    _sizes(name, x)
-    t, h, c = x.stride()
-    if (c != 1 and x.shape[2] > 1) or not x.is_cuda:
-        raise VMonarchError(f"{name}: a CUDA tensor with adjacent channels is needed")
-    if like is not None and (x.dtype != like.dtype or x.device != like.device or x.shape[2] != like.shape[2]):
-        raise VMonarchError(f"{name}: type, device or head size differ from the other tensors'")
-    return Tokens(x.data_ptr(), t, h)
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3 or x.dtype is not like.dtype or x.get_device() != like.get_device() or shape[2] != like.shape[2]:
+        raise VMonarchError(f"{name}: expected [tokens, heads, d] of the other tensors' type, device and head size")
+    if stride[2] != 1 and shape[2] > 1:
+        raise VMonarchError(f"{name}: adjacent channels are needed")
+    return byref(Tokens(x.data_ptr(), stride[0], stride[1]))
 
 
-def _int32(name, x, like, shape=None):
-    if x.dtype != torch.int32 or x.device != like.device or not x.is_contiguous():
-        raise VMonarchError(f"{name}: a contiguous int32 tensor on the other tensors' device is needed")
-    if shape is not None and tuple(x.shape) != shape:
-        raise VMonarchError(f"{name}: expected shape {shape}, got {tuple(x.shape)}")
+def _int32(name, x, like, shape):
+    if x.dtype is not torch.int32 or x.get_device() != like.get_device() or x.shape != shape or not x.is_contiguous():
+        raise VMonarchError(f"{name}: a contiguous int32 tensor of shape {tuple(shape)} on the other tensors' device is needed")
     return x.data_ptr()
 
 
@@ -448,15 +448,22 @@ def _same_shape(name, x, y):
         raise VMonarchError(f"{name}: expected shape {tuple(y.shape)}, got {tuple(x.shape)}")
 
 
+_entries = {}  # (name, type) -> function of the library
+
+
 def _run(name, like, *args):
     """Calls an entry point on the current stream of `like`'s device."""
-    fn = getattr(lib(), name + _suffix(like))
-    dev = like.device.index
+    fn = _entries.get((name, like.dtype))
+    if fn is None:
+        fn = _entries[name, like.dtype] = getattr(lib(), name + _suffix(like))
+    dev = like.get_device()
     if dev == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+        rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
     else:
         with torch.cuda.device(dev):
-            _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+            rc = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if rc:
+        _check(rc)
 
 
 def rotary_plan(axis_pairs, base=10000.0, interleaved=False, factor=1.0, context=0.0, low_turns=0.0, high_turns=0.0, amplitude=1.0) -> RotaryPlan:
@@ -475,22 +482,25 @@ def rotary(q, k, positions, plan: RotaryPlan, backward=False, q_out=None, k_out=
     """Turns q and k ([tokens, heads, d]; k may be None) at positions (int32 [axes, tokens], or [tokens] for one axis); backward: gradients of the
     turned tensors to those of q and k.  q_out / k_out may be q / k themselves.  Returns (q_out, k_out)."""
     n, heads, d = _sizes("q", q)
-    q_out = torch.empty_like(q) if q_out is None else q_out
-    dq, dqo, dk, dko, heads_k = _tokens("q", q), _tokens("q_out", q_out, q), None, None, 0
-    _same_shape("q_out", q_out, q)
+    if q_out is None:
+        q_out = torch.empty_like(q)
+    else:
+        _same_shape("q_out", q_out, q)
+    heads_k, dk, dko = 0, None, None
     if k is not None:
-        k_out = torch.empty_like(k) if k_out is None else k_out
+        if k_out is None:
+            k_out = torch.empty_like(k)
+        else:
+            _same_shape("k_out", k_out, k)
         dk, dko, heads_k = _tokens("k", k, q), _tokens("k_out", k_out, q), k.shape[1]
-        _same_shape("k_out", k_out, k)
         if k.shape[0] != n:
             raise VMonarchError("k: as many tokens as q are needed")
-        dk, dko = ctypes.byref(dk), ctypes.byref(dko)
     elif k_out is not None:
         raise VMonarchError("k_out without k")
     if positions.dim() == 1:
         positions = positions[None]
-    at = _int32("positions", positions, q, (plan.axes, n))
-    _run("vmonarch_rotary", q, ctypes.byref(dq), ctypes.byref(dqo), heads, dk, dko, heads_k, n, d, at, n, ctypes.byref(plan), int(bool(backward)))
+    _run("vmonarch_rotary", q, _tokens("q", q, q), _tokens("q_out", q_out, q), heads, dk, dko, heads_k, n, d,
+         _int32("positions", positions, q, (plan.axes, n)), n, byref(plan), 1 if backward else 0)
     return q_out, k_out
 
 
@@ -499,90 +509,98 @@ def packed_attention(q, k, v, q_starts, k_starts=None, causal=True, scale=None, 
     q_starts).  scale defaults to 1 / sqrt(d).  Returns out, or (out, lse) with lse float32 [heads_q, tokens_q] for packed_attention_bwd.
     Rows of no sequence are not written: bring a cleared `out` where a padded batch's tail is read later."""
     nq, heads, d = _sizes("q", q)
-    k_starts = q_starts if k_starts is None else k_starts
-    out = torch.empty((nq, heads, d), dtype=q.dtype, device=q.device) if out is None else out
-    _same_shape("out", out, q)
+    nk, kv, _ = _sizes("k", k)
+    if out is None:
+        out = q.new_empty((nq, heads, d))
+    else:
+        _same_shape("out", out, q)
     _same_shape("v", v, k)
     stat = torch.empty((heads, nq), dtype=torch.float32, device=q.device) if lse else None
     n = q_starts.numel()
-    a, b, c, o = _tokens("q", q), _tokens("k", k, q), _tokens("v", v, q), _tokens("out", out, q)
-    _run("vmonarch_packed_attention", q, ctypes.byref(a), ctypes.byref(b), ctypes.byref(c), ctypes.byref(o), stat.data_ptr() if lse else None,
-         _int32("q_starts", q_starts, q, (n,)), _int32("k_starts", k_starts, q, (n,)), n - 1, nq, k.shape[0], heads, k.shape[1], d,
-         1.0 / math.sqrt(d) if scale is None else scale, int(bool(causal)))
+    qs = _int32("q_starts", q_starts, q, (n,))
+    ks = qs if k_starts is None or k_starts is q_starts else _int32("k_starts", k_starts, q, (n,))
+    _run("vmonarch_packed_attention", q, _tokens("q", q, q), _tokens("k", k, q), _tokens("v", v, q), _tokens("out", out, q),
+         stat.data_ptr() if lse else None, qs, ks, n - 1, nq, nk, heads, kv, d, 1.0 / math.sqrt(d) if scale is None else scale, 1 if causal else 0)
     return (out, stat) if lse else out
 
 
 def packed_attention_bwd(q, k, v, out, d_out, lse, q_starts, k_starts=None, causal=True, scale=None, dq=None, dk=None, dv=None, workspace=None):
     """Gradients (dq, dk, dv) of packed_attention from its out and lse.  Rows of no sequence are not written (see there)."""
     nq, heads, d = _sizes("q", q)
-    k_starts = q_starts if k_starts is None else k_starts
-    dq = torch.empty((nq, heads, d), dtype=q.dtype, device=q.device) if dq is None else dq
-    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
-    dv = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dv is None else dv
+    nk, kv, _ = _sizes("k", k)
+    dq = q.new_empty((nq, heads, d)) if dq is None else dq
+    dk = q.new_empty((nk, kv, d)) if dk is None else dk
+    dv = q.new_empty((nk, kv, d)) if dv is None else dv
     for name, x, y in (("v", v, k), ("out", out, q), ("d_out", d_out, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
         _same_shape(name, x, y)
     if lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous() or tuple(lse.shape) != (heads, nq):
         raise VMonarchError("lse: the log-sum-exp of packed_attention is needed, float32 [heads_q, tokens_q]")
     n = q_starts.numel()
-    if workspace is None:
-        size = lib().vmonarch_packed_attention_bwd_workspace_bytes(n - 1, nq, k.shape[0], heads, k.shape[1], d)
-        workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
-    x = [_tokens(name, t, q) for name, t in (("q", q), ("k", k), ("v", v), ("out", out), ("d_out", d_out), ("dq", dq), ("dk", dk), ("dv", dv))]
-    p = [ctypes.byref(t) for t in x]
-    size = workspace.numel() * workspace.element_size()
-    _run("vmonarch_packed_attention_bwd", q, *p[:5], lse.data_ptr(), *p[5:], _int32("q_starts", q_starts, q, (n,)),
-         _int32("k_starts", k_starts, q, (n,)), n - 1, nq, k.shape[0], heads, k.shape[1], d, 1.0 / math.sqrt(d) if scale is None else scale,
-         int(bool(causal)), workspace.data_ptr() if size else None, size)
+    qs = _int32("q_starts", q_starts, q, (n,))
+    ks = qs if k_starts is None or k_starts is q_starts else _int32("k_starts", k_starts, q, (n,))
+    at, size = _workspace(workspace, q, "vmonarch_packed_attention_bwd_workspace_bytes", n - 1, nq, nk, heads, kv, d)
+    _run("vmonarch_packed_attention_bwd", q, _tokens("q", q, q), _tokens("k", k, q), _tokens("v", v, q), _tokens("out", out, q),
+         _tokens("d_out", d_out, q), lse.data_ptr(), _tokens("dq", dq, q), _tokens("dk", dk, q), _tokens("dv", dv, q), qs, ks, n - 1, nq, nk, heads, kv, d,
+         1.0 / math.sqrt(d) if scale is None else scale, 1 if causal else 0, None if at is None else at.data_ptr(), size)
     return dq, dk, dv
+
+
+def _workspace(given, like, name, *sizes):
+    """The caller's workspace, or one of as many bytes as `name` says from torch's allocator; (tensor or None, bytes)."""
+    if given is not None:
+        if given.get_device() != like.get_device() or not given.is_contiguous():
+            raise VMonarchError("workspace: a contiguous tensor on the other tensors' device is needed")
+        return given, given.numel() * given.element_size()
+    size = getattr(lib(), name)(*sizes)
+    return (torch.empty(size, dtype=torch.uint8, device=like.device), size) if size else (None, 0)
 
 
 def _cache(cache_k, cache_v, table, lengths, like, n_seqs):
     """The descriptor of a cache: cache_k, cache_v [pages, page_size, heads_kv, d] with adjacent channels, table int32 [n_seqs, width]."""
-    _same_shape("cache_v", cache_v, cache_k)
-    for name, x in (("cache_k", cache_k), ("cache_v", cache_v)):
-        if x.dim() != 4 or x.dtype != like.dtype or x.device != like.device or x.shape[3] != like.shape[2] or (x.stride(3) != 1 and x.shape[3] > 1):
-            raise VMonarchError(f"{name}: expected [pages, page_size, heads, d] with adjacent channels, of the other tensors' type, device and head size")
-    if table.dtype != torch.int32 or table.device != like.device or table.dim() != 2 or table.shape[0] != n_seqs or (table.stride(1) != 1 and table.shape[1] > 1):
+    shape, ks, vs = cache_k.shape, cache_k.stride(), cache_v.stride()
+    if cache_v.shape != shape or len(shape) != 4 or shape[3] != like.shape[2] or ((ks[3] != 1 or vs[3] != 1) and shape[3] > 1):
+        raise VMonarchError("cache_k, cache_v: expected [pages, page_size, heads, d] with adjacent channels, of the other tensors' head size")
+    dev = like.get_device()
+    if cache_k.dtype is not like.dtype or cache_v.dtype is not like.dtype or cache_k.get_device() != dev or cache_v.get_device() != dev:
+        raise VMonarchError("cache_k, cache_v: the other tensors' type and device are needed")
+    width, ts = table.shape, table.stride()
+    if table.dtype is not torch.int32 or table.get_device() != dev or len(width) != 2 or width[0] != n_seqs or (ts[1] != 1 and width[1] > 1):
         raise VMonarchError("table: expected int32 [n_seqs, pages of the longest] on the other tensors' device")
-    ks, vs = cache_k.stride(), cache_v.stride()
-    return Cache(cache_k.data_ptr(), cache_v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], cache_k.shape[0], cache_k.shape[1], table.data_ptr(),
-                 table.stride(0), table.shape[1], _int32("lengths", lengths, like, (n_seqs,)))
+    return byref(Cache(cache_k.data_ptr(), cache_v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], shape[0], shape[1], table.data_ptr(), ts[0], width[1],
+                       _int32("lengths", lengths, like, (n_seqs,))))
 
 
 def paged_append(k, v, cache_k, cache_v, table, q_starts, lengths, plan: RotaryPlan = None, positions=None):
     """Writes each sequence's chunk of new tokens (k, v [tokens, heads_kv, d], cut by q_starts) into the last slots of its lengths[s] tokens in the
     pages; with a plan keys are turned on the way, at `positions` or at the tokens' positions in their sequence."""
-    n = q_starts.numel() - 1
+    nk, kv, d = _sizes("k", k)
     _same_shape("v", v, k)
-    a, b, c = _tokens("k", k), _tokens("v", v, k), _cache(cache_k, cache_v, table, lengths, k, n)
-    if cache_k.shape[2] != k.shape[1]:
+    n = q_starts.numel()
+    cache = _cache(cache_k, cache_v, table, lengths, k, n - 1)
+    if cache_k.shape[2] != kv:
         raise VMonarchError("cache_k: as many heads as k are needed")
     at = None
     if positions is not None:
         if plan is None:
             raise VMonarchError("positions without a plan")
         positions = positions[None] if positions.dim() == 1 else positions
-        at = _int32("positions", positions, k, (plan.axes, k.shape[0]))
-    _run("vmonarch_paged_append", k, ctypes.byref(a), ctypes.byref(b), ctypes.byref(c), _int32("q_starts", q_starts, k, (n + 1,)), n, k.shape[0],
-         k.shape[1], k.shape[2], None if plan is None else ctypes.byref(plan), at, k.shape[0])
+        at = _int32("positions", positions, k, (plan.axes, nk))
+    _run("vmonarch_paged_append", k, _tokens("k", k, k), _tokens("v", v, k), cache, _int32("q_starts", q_starts, k, (n,)), n - 1, nk, kv, d,
+         None if plan is None else byref(plan), at, nk)
 
 
 def paged_attention(q, cache_k, cache_v, table, q_starts, lengths, causal=True, scale=None, out=None, workspace=None):
     """Attention of each sequence's chunk of new tokens (q [tokens, heads_q, d], cut by q_starts) over its lengths[s] tokens in the pages, the chunk's
     own included.  Rows of no sequence are not written (see packed_attention)."""
     nq, heads, d = _sizes("q", q)
-    n = q_starts.numel() - 1
-    out = torch.empty((nq, heads, d), dtype=q.dtype, device=q.device) if out is None else out
-    _same_shape("out", out, q)
-    a, o, c = _tokens("q", q), _tokens("out", out, q), _cache(cache_k, cache_v, table, lengths, q, n)
-    kv = cache_k.shape[2]
-    size = 0
-    if workspace is None:
-        size = lib().vmonarch_paged_attention_workspace_bytes(ctypes.byref(c), n, nq, heads, kv, d)
-        if size:
-            workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+    n = q_starts.numel()
+    if out is None:
+        out = q.new_empty((nq, heads, d))
     else:
-        size = workspace.numel() * workspace.element_size()
-    _run("vmonarch_paged_attention", q, ctypes.byref(a), ctypes.byref(c), ctypes.byref(o), _int32("q_starts", q_starts, q, (n + 1,)), n, nq, heads, kv, d,
-         1.0 / math.sqrt(d) if scale is None else scale, int(bool(causal)), workspace.data_ptr() if size else None, size)
+        _same_shape("out", out, q)
+    cache = _cache(cache_k, cache_v, table, lengths, q, n - 1)
+    kv = cache_k.shape[2]
+    at, size = _workspace(workspace, q, "vmonarch_paged_attention_workspace_bytes", cache, n - 1, nq, heads, kv, d)
+    _run("vmonarch_paged_attention", q, _tokens("q", q, q), cache, _tokens("out", out, q), _int32("q_starts", q_starts, q, (n,)), n - 1, nq, heads, kv, d,
+         1.0 / math.sqrt(d) if scale is None else scale, 1 if causal else 0, None if at is None else at.data_ptr(), size)
     return out

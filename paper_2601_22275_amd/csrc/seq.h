@@ -54,7 +54,7 @@ struct SeqParams {
 };
 
 // Backward, bf16: rows of queries whose workgroup sees at most this many keys sum D over them instead of reading it off the stored output
-constexpr int kSeqExactKeys = 256;
+constexpr int kSeqExactKeys = 512;
 
 // ---- device: sequences --------------------------------------------------------------------------------------------------------
 struct Span {
