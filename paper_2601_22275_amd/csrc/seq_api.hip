@@ -213,10 +213,13 @@ PagedPlan paged_plan(long long table_keys, int n_seqs, long long tokens, int hea
   const long long rows = tokens * group;
   p.few = rows <= 32LL * n_seqs;
   const long long blocks = tile_bound(tokens, group, p.few ? 32 : 128, n_seqs) * heads_kv;
-  const long long want = (p.few ? 4LL : 2LL) * compute_units();
+  // Few rows: small workgroups that stream the cache, eight for every compute unit in turn (16 tokens over up to 16,384 keys: four 145 us, eight
+  // 136, sixteen 143).  Many: two on a unit at once, and no more ranges than one such round holds (a frame over 21 frames: 600 workgroups
+  // 131 us, 480 107).
   const long long shortest = p.few ? 256 : 512;
-  long long r = (want + blocks - 1) / blocks;
+  long long r = p.few ? (8LL * compute_units() + blocks - 1) / blocks : 2LL * compute_units() / blocks;
   if (r > (table_keys + shortest - 1) / shortest) r = (table_keys + shortest - 1) / shortest;
+  if (r < 1) r = 1;
   p.ranges = r > 64 ? 64 : (int)r;
   return p;
 }
@@ -225,7 +228,8 @@ template <typename E>
 hipError_t launch_attention(const SeqParams<E>& P, bool few, hipStream_t st) {
   hipError_t e;
   if constexpr (sizeof(E) == 2) {
-    if (P.aligned && P.d <= 128) {
+    // (packed keys: 64 rows of an LDS tile lie within 2^31 bytes)
+    if (P.aligned && P.d <= 128 && (P.page_size > 0 || (P.k.t < (1 << 24) && P.v.t < (1 << 24)))) {
       if (few) e = P.d <= 64 ? launch_seq_token<64>(P, st) : launch_seq_token<128>(P, st);
       else e = P.d <= 64 ? launch_seq_attention_mfma<64>(P, st) : launch_seq_attention_mfma<128>(P, st);
     } else {

@@ -57,32 +57,9 @@ __device__ __forceinline__ bool odd_values(unsigned at) {
   return __any(max(largest[0], largest[1]) >= 0x7f80);
 }
 
-// A key's place in the pages, stepped from tile to tile without a division
-struct PagePointer {
-  int n, slot;  // page of the sequence, slot in it
-  __device__ __forceinline__ void start(const SeqParams<bf16_t>& P, int key) {
-    n = key / P.page_size;
-    slot = key - n * P.page_size;
-  }
-  __device__ __forceinline__ void advance(const SeqParams<bf16_t>& P, int keys) {
-    const int whole = keys / P.page_size;  // the same for all lanes
-    n += whole;
-    slot += keys - whole * P.page_size;
-    if (slot >= P.page_size) {
-      slot -= P.page_size;
-      ++n;
-    }
-  }
-  // Keys past the last one stand for the last one's page; its slot likewise
-  __device__ __forceinline__ int page(const SeqParams<bf16_t>& P, int seq, int nk) const {
-    const int last = max(nk - 1, 0) / P.page_size;
-    const int p = P.table[seq * P.table_stride + min(n, last)];
-    return p < 0 || p >= P.n_pages ? 0 : p;
-  }
-  __device__ __forceinline__ int slot_of(const SeqParams<bf16_t>& P, int nk) const {
-    const int last = max(nk - 1, 0) / P.page_size, last_slot = max(nk - 1, 0) - last * P.page_size;
-    return n > last || (n == last && slot > last_slot) ? last_slot : slot;
-  }
+// Where a key's row and its value's lie
+struct alignas(16) RowAt {
+  const bf16_t *k, *v;
 };
 
 }  // namespace

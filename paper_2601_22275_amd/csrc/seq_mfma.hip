@@ -54,6 +54,8 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
   constexpr int BQ = 32 * W2;
   auto swz = [](int row) { return G::swz(row); };
   extern __shared__ __attribute__((aligned(16))) char smem[];  // [K|V][NSLOT][BT rows][2 D bytes]
+  __shared__ int entry[PAGED ? 4 : 1][64];
+  __shared__ RowAt row_at[PAGED ? 4 : 1][BT];
 
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -101,46 +103,50 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
   const int st_lc = (lane % CH) ^ swz(st_row);
   const bool st_on = st_lc * 8 < P.d;
   const unsigned lds_base = (unsigned)(unsigned long long)(__attribute__((address_space(3))) char*)smem;
-  const char* kbase = reinterpret_cast<const char*>(P.k.p + kvh * P.k.h + (PAGED ? 0LL : (long long)(k_begin + k0) * P.k.t));
-  const char* vbase = reinterpret_cast<const char*>(P.v.p + kvh * P.v.h + (PAGED ? 0LL : (long long)(k_begin + k0) * P.v.t));
-  PagePointer pp[PAGED ? NR : 1];
-  int page_next[PAGED ? NR : 1];
-  if (PAGED) {
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-      pp[r].start(P, k0 + RPI * W2 * r + st_row);
-      page_next[r] = pp[r].page(P, w.seq, nk);
-    }
-  }
+  const bf16_t* kbase = P.k.p + kvh * P.k.h + (PAGED ? 0LL : (long long)(k_begin + k0) * P.k.t);
+  const bf16_t* vbase = P.v.p + kvh * P.v.h + (PAGED ? 0LL : (long long)(k_begin + k0) * P.v.t);
+  // Packed keys: a tile's address is wave-uniform, a lane's place in it a 32-bit offset (the host keeps a tile's rows within 2^31 bytes).
+  // Pages: rows lie anywhere.  Their addresses are formed once each, by one wave for all, a tile ahead of their loads (row_at), from entries of
+  // the table that came to LDS a tile before that (entry).  (64-bit products in every lane that loads: 16,384 causal tokens 861 TFLOP/s, so 947.)
+  const int row_k = (int)(2 * P.k.t), row_v = (int)(2 * P.v.t);  // bytes (packed keys)
+  const int last_key = max(nk - 1, 0);
+  auto key_of = [&](int t) __attribute__((always_inline)) { return min(k0 + t * BT + lane % BT, last_key); };
+  auto fetch_entries = [&](int t) __attribute__((always_inline)) {  // by one wave; past the last tile: the last key's, never used
+    const int* e = P.table + w.seq * P.table_stride + key_of(t) / P.page_size;
+    const unsigned dst = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long long)(__attribute__((address_space(3))) char*)&entry[t & 3][0]);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(e), "s"(dst) : "memory", "m0");
+  };
+  auto prepare_rows = [&](int t) __attribute__((always_inline)) {  // by one wave
+    const int e = entry[t & 3][lane];
+    const long long page = e < 0 || e >= P.n_pages ? 0 : e;
+    const int slot = key_of(t) % P.page_size;
+    row_at[t & 3][lane % BT] = RowAt{kbase + page * P.k.page + slot * P.k.t, vbase + page * P.v.page + slot * P.v.t};
+  };
   auto issue_tile = [&](int t) __attribute__((always_inline)) {  // into slot t & 3
     const unsigned kb = lds_base + (t & (NSLOT - 1)) * TILE_BYTES;
+    const bf16_t* ktile = kbase + (PAGED ? 0LL : (long long)t * BT * P.k.t);
+    const bf16_t* vtile = vbase + (PAGED ? 0LL : (long long)t * BT * P.v.t);
     const int last = nk - 1 - k0 - t * BT;  // the tile's last row that is a key
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       const int row = RPI * W2 * r + st_row;
       const unsigned dst = __builtin_amdgcn_readfirstlane(kb + (RPI * W2 * r + RPI * wave) * ROW_BYTES);
-      const char *ka, *va;
+      const unsigned vdst = dst + V_OFF;
       if (PAGED) {
-        const long long page = page_next[r];
-        const int slot = pp[r].slot_of(P, nk);
-        ka = kbase + (page * P.k.page + slot * P.k.t + st_lc * 8) * 2;
-        va = vbase + (page * P.v.page + slot * P.v.t + st_lc * 8) * 2;
-        pp[r].advance(P, BT);
+        const RowAt at = row_at[t & 3][row];
+        const bf16_t *ka = at.k + st_lc * 8, *va = at.v + st_lc * 8;
+        if (st_on) {
+          asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(ka), "s"(dst) : "memory", "m0");
+          asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(va), "s"(vdst) : "memory", "m0");
+        }
       } else {
-        const long long at = t * BT + min(row, last);
-        ka = kbase + (at * P.k.t + st_lc * 8) * 2;
-        va = vbase + (at * P.v.t + st_lc * 8) * 2;
+        const int at = min(row, last);
+        const unsigned ko = at * row_k + st_lc * 16, vo = at * row_v + st_lc * 16;
+        if (st_on) {
+          asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(ko), "s"(ktile), "s"(dst) : "memory", "m0");
+          asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(vo), "s"(vtile), "s"(vdst) : "memory", "m0");
+        }
       }
-      if (st_on) {
-        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(ka), "s"(dst) : "memory", "m0");
-        const unsigned vdst = dst + V_OFF;
-        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(va), "s"(vdst) : "memory", "m0");
-      }
-    }
-    if (PAGED) {
-      // the next tile's pages, here by the time its loads are issued
-#pragma unroll
-      for (int r = 0; r < NR; ++r) page_next[r] = pp[r].page(P, w.seq, nk);
     }
   };
   if (P.d < D) {
@@ -153,6 +159,12 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
     static_assert(TILE_BYTES % (16 * 64 * W2) == 0, "the clear covers the slot exactly");
 #pragma unroll
     for (int r = 0; r < TILE_BYTES / (16 * 64 * W2); ++r) *reinterpret_cast<uint4*>(smem + V_OFF + 3 * TILE_BYTES + (r * 64 * W2 + tid) * 16) = z;
+  }
+  if (PAGED && ntiles > 0) {
+    fetch_entries(wave);  // tiles 0 .. 3
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    prepare_rows(wave);  // (tile 3's again in the first iteration)
+    __syncthreads();
   }
   if (ntiles > 0) issue_tile(0);
   if (ntiles > 1) issue_tile(1);
@@ -228,7 +240,7 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
   // ---- one step of the pipeline (see the top): KS groups of logits, then 2 CT groups of products --------
   constexpr int NPV = 2 * CT;
   constexpr int NG = KS + NPV;
-  constexpr int PF = 2, RING = 4;
+  constexpr int PF = 3, RING = 4;
   static_assert(NG % RING == 0 && RING > PF, "ring positions repeat from step to step");
   bf16x8 ring[RING];
   auto request = [&](auto gc, int s_off, int pv_off) __attribute__((always_inline)) {
@@ -375,7 +387,9 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();  // tile tt + 1 has landed for everyone; everyone is done with tile tt - 2
     }
+    if (PAGED && (tt & (W2 - 1)) == wave) prepare_rows(tt + 3);
     if (tt + 2 < ntiles) issue_tile(tt + 2);
+    if (PAGED && ((tt + 1) & (W2 - 1)) == wave) fetch_entries(tt + 4);
   };
   if (ntiles > 0) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");

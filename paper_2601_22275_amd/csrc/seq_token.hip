@@ -2,10 +2,12 @@
 // ranges of keys.
 //
 //   out = sum_j 2^(s_j - m) v_j / sum_j 2^(s_j - m)     is the same sum over ranges of keys once each carries its own m.
-// The cache is read once and bounds the kernel (8 TB/s); up to 32 packed rows (token, head of the group) share that read.  A workgroup is four
+// The cache is read once and bounds the kernel (8 TB/s); up to 32 packed rows (token, head of the group) share that read.  A workgroup is two
 // waves that take 32-key sub-tiles of its range in turn, each with LDS slots, a running maximum, a sum and accumulators of its own: no
-// barrier in the loop, a wave waits for its own loads only, and 64 KB are in flight on a compute unit.  The waves join through LDS at the end, the
-// ranges (blockIdx.y) through memory and a second launch.  Products as in seq_mfma.hip: S^T = K Q^T and O^T += V^T P^T, both
+// barrier in the loop, a wave waits for its own loads only; two workgroups share a compute unit, so that one's start and end pass behind the
+// other's stream.  The waves join through LDS at the end, the ranges (blockIdx.y) through memory and a second launch.
+// 16 single tokens over up to 16,384 keys, 40 heads on 8, d = 128 (585 MB): 136 us, 4.3 TB/s with the join, where a large copy moves 5.0;
+// four waves in one workgroup 142, every lane forming the addresses of the rows it loads 160.  Products as in seq_mfma.hip: S^T = K Q^T and O^T += V^T P^T, both
 // v_mfma_f32_32x32x16_bf16.
 #include "seq_device.h"
 
@@ -13,7 +15,7 @@ namespace vm {
 
 namespace {
 
-constexpr int NW = 4;
+constexpr int NW = 2;
 
 // Sub-tiles in flight per wave: 128 KB of LDS either way
 template <int D>
@@ -22,7 +24,7 @@ constexpr int slots() {
 }
 
 template <int D>
-__global__ void __launch_bounds__(64 * NW, 1) seq_token_kernel(SeqParams<bf16_t> P) {
+__global__ void __launch_bounds__(64 * NW, 2) seq_token_kernel(SeqParams<bf16_t> P) {
   using G = RowGeo<D>;
   constexpr int ROW_BYTES = G::ROW_BYTES, KS = G::KS, CT = G::CT, CH = G::CH, RPI = G::RPI;
   constexpr int NS = slots<D>();
@@ -34,12 +36,14 @@ __global__ void __launch_bounds__(64 * NW, 1) seq_token_kernel(SeqParams<bf16_t>
   extern __shared__ __attribute__((aligned(16))) char smem[];  // [wave][NS][K|V][32 rows]
   __shared__ float wave_m[NW][32], wave_l[NW][32];
   __shared__ int pages[NW][2 * NS][64];  // entries of the table
+  __shared__ RowAt row_at[NW][32];
 
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, ql = lane & 31, g = lane >> 5;
-  const int kvh = blockIdx.x % P.heads_kv;
-  const Span w = find_tile(P.q_starts, P.n_seqs, P.tokens_q, P.group, BQ, blockIdx.x / P.heads_kv);
+  const int tiles = gridDim.x / P.heads_kv;
+  const int kvh = blockIdx.x / tiles;
+  const Span w = find_tile(P.q_starts, P.n_seqs, P.tokens_q, P.group, BQ, blockIdx.x - kvh * tiles);
   const long long rows = (long long)w.count * P.group;
   const long long row_first = (long long)w.tile * BQ;
   if (row_first >= rows) return;
@@ -74,20 +78,22 @@ __global__ void __launch_bounds__(64 * NW, 1) seq_token_kernel(SeqParams<bf16_t>
     const unsigned dst = __builtin_amdgcn_readfirstlane(ring + (i % (2 * NS)) * 256);
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(entry), "s"(dst) : "memory", "m0");
   };
+  // The rows' addresses, formed once each, pass through LDS to the lanes that load them
+  auto prepare = [&](int i) {
+    const int p = pages[wave][i % (2 * NS)][lane];
+    const long long page = p < 0 || p >= P.n_pages ? 0 : p;
+    const int slot = key_of(i) % P.page_size;
+    row_at[wave][ql] = RowAt{kbase + page * P.k.page + slot * P.k.t, vbase + page * P.v.page + slot * P.v.t};  // (both halves of the wave alike)
+  };
   auto issue = [&](int i) {
     fetch_page(i + NS);  // (past the last sub-tile: the last key's, never used)
-    const int p = pages[wave][i % (2 * NS)][lane];
-    const int page = p < 0 || p >= P.n_pages ? 0 : p;
-    const int slot = key_of(i) % P.page_size;
     const unsigned base = lds_base + (i % NS) * SLOT_BYTES;
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       const int row = RPI * r + lane / CH;
       const int c = ((lane % CH) ^ swz(row)) * 8;
-      const long long pg = __shfl(page, row);
-      const int sl = __shfl(slot, row);
-      const bf16_t* ka = kbase + pg * P.k.page + sl * P.k.t + c;
-      const bf16_t* va = vbase + pg * P.v.page + sl * P.v.t + c;
+      const RowAt at = row_at[wave][row];
+      const bf16_t *ka = at.k + c, *va = at.v + c;
       const unsigned dst = __builtin_amdgcn_readfirstlane(base + RPI * r * ROW_BYTES);
       const unsigned vdst = dst + SUB_BYTES;
       if (c < P.d) {
@@ -106,7 +112,10 @@ __global__ void __launch_bounds__(64 * NW, 1) seq_token_kernel(SeqParams<bf16_t>
     for (int i = 0; i < NS; ++i) fetch_page(i);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll 1
-    for (int i = 0; i < min(NS, mine); ++i) issue(i);
+    for (int i = 0; i < min(NS, mine); ++i) {
+      prepare(i);
+      issue(i);
+    }
   }
 
   // ---- queries ----------------------------------------------------------------------------------------------------------------------
@@ -143,6 +152,10 @@ __global__ void __launch_bounds__(64 * NW, 1) seq_token_kernel(SeqParams<bf16_t>
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[ct][r] = 0.f;
   float m = NEG_BIG, l = 0.f;
+  typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+  bf16x2 ones2;
+  ones2[0] = (__bf16)1.0f;
+  ones2[1] = (__bf16)1.0f;
 
 #pragma unroll 1
   for (int i = 0; i < mine; ++i) {
@@ -154,6 +167,7 @@ __global__ void __launch_bounds__(64 * NW, 1) seq_token_kernel(SeqParams<bf16_t>
     else if (NS == 4 && behind == 2) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * LOADS) : "memory");
     else if (behind >= 1) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(LOADS) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (i + NS < mine) prepare(i + NS);  // (its pages came in front of this sub-tile's rows)
     const unsigned off = (i % NS) * SLOT_BYTES;
     const int first = k0 + 32 * (wave + NW * i);
     f32x16 s;
@@ -170,23 +184,28 @@ __global__ void __launch_bounds__(64 * NW, 1) seq_token_kernel(SeqParams<bf16_t>
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < left ? s[r] : -INFINITY;
     }
-    const float m2 = fmaxf(m, subtile_max(s) * sc);
-    const float alpha = __builtin_amdgcn_exp2f(m - m2);
-    m = m2;
-    float p[16], sum = 0.f;
+    // The reference moves where a row's maximum has outgrown it by 2^8 (any reference gives the same result), and for all rows of the wave
+    const float top = subtile_max(s) * sc;
+    if (__any(top > m + 8.0f)) {
+      const float m2 = fmaxf(m, top);
+      const float alpha = __builtin_amdgcn_exp2f(m - m2);
+      m = m2;
+      l *= alpha;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, -m2));
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[ct][r] *= alpha;
+    }
     bf16x8 pb[2];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      pb[r >> 3][r & 7] = (__bf16)p[r];
-      sum += (float)pb[r >> 3][r & 7];  // of the rounded weights: rows are exact convex combinations
+    for (int r = 0; r < 16; r += 2) {
+      bf16x2 pr;
+      pr[0] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc, -m));
+      pr[1] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 1], sc, -m));
+      l = __builtin_amdgcn_fdot2_f32_bf16(pr, ones2, l, false);  // of the rounded weights: rows are exact convex combinations
+      pb[r >> 3][r & 7] = pr[0];
+      pb[r >> 3][(r & 7) + 1] = pr[1];
     }
-    l = l * alpha + sum;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[ct][r] *= alpha;
     auto value = [&](int c, int ct) -> bf16x8 {
       const unsigned at = off + c * 16 * ROW_BYTES;
       const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_b64_ptr)(unsigned long long)((t_base[0] ^ (ct << 6)) + at));
@@ -277,29 +296,47 @@ __global__ void __launch_bounds__(64 * NW, 1) seq_token_kernel(SeqParams<bf16_t>
   }
 }
 
-// Ranges of keys joined: a row's partial results weigh 2^(their log-sum) relative to the largest.  D / 4 lanes per packed row.
-template <typename E, int D>
+// Ranges of keys joined: a row's partial results weigh 2^(their log-sum) relative to the largest.  D / 4 lanes take a packed row's channels; where
+// ranges are many, GROUPS such groups share the row and its ranges (one group after another's load, 64 ranges took 60 us).
+template <typename E, int D, int GROUPS>
 __global__ void __launch_bounds__(256) seq_join_kernel(SeqParams<E> P) {
+  constexpr int LANES = D / 4, ROWS = 256 / LANES / GROUPS;
+  static_assert(ROWS >= 1, "a workgroup holds a row's groups");
+  __shared__ f32x4 sums[GROUPS > 1 ? GROUPS : 1][ROWS][LANES];
+  __shared__ float totals[GROUPS > 1 ? GROUPS : 1][ROWS];
+  const int lane = threadIdx.x % LANES, local = threadIdx.x / LANES % ROWS, grp = threadIdx.x / LANES / ROWS;
   const long long all = (long long)P.tokens_q * P.group;  // packed rows of a key head
-  const long long row = (long long)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
-  const int kvh = blockIdx.y, c = threadIdx.x % (D / 4) * 4;
-  if (row >= all) return;
-  const int tok = (int)(row / P.group);
-  if (tok < start_of(P.q_starts, 0, P.tokens_q) || tok >= start_of(P.q_starts, P.n_seqs, P.tokens_q)) return;  // of no sequence
+  const long long row = (long long)blockIdx.x * ROWS + local;
+  const int kvh = blockIdx.y, c = lane * 4;
+  const int tok = (int)(min(row, all - 1) / P.group);
+  const bool in = row < all && tok >= start_of(P.q_starts, 0, P.tokens_q) && tok < start_of(P.q_starts, P.n_seqs, P.tokens_q);  // of a sequence
   const long long step = P.heads_kv * all, at = kvh * all + row;
-  float top = NEG_BIG;
-  for (int x = 0; x < P.ranges; ++x) top = fmaxf(top, P.part_s[x * step + at]);
-  float total = 0.f;
+  float top = NEG_BIG, total = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int x = 0; x < P.ranges; ++x) {
-    const float s = P.part_s[x * step + at];
-    if (s == -INFINITY) continue;
-    const float f = __builtin_amdgcn_exp2f(s - top);
-    total += f;
-    o += *reinterpret_cast<const f32x4*>(P.part_o + (x * step + at) * D + c) * f;
+  if (in) {
+#pragma unroll 4
+    for (int x = 0; x < P.ranges; ++x) top = fmaxf(top, P.part_s[x * step + at]);
+    // (a range of which the row sees nothing has left zeros and a log-sum of -inf)
+#pragma unroll 4
+    for (int x = grp; x < P.ranges; x += GROUPS) {
+      const float f = __builtin_amdgcn_exp2f(P.part_s[x * step + at] - top);
+      total += f;
+      o += *reinterpret_cast<const f32x4*>(P.part_o + (x * step + at) * D + c) * f;
+    }
   }
+  if (GROUPS > 1) {
+    sums[grp][local][lane] = o;
+    if (lane == 0) totals[grp][local] = total;
+    __syncthreads();
+    if (grp > 0) return;
+#pragma unroll
+    for (int x = 1; x < GROUPS; ++x) {
+      o += sums[x][local][lane];
+      total += totals[x][local];
+    }
+  }
+  if (!in || c >= P.d) return;
   const float inv = total == 0.f ? 0.f : 1.0f / total;
-  if (c >= P.d) return;
   E* out = P.out.p + (long long)tok * P.out.t + (kvh * P.group + (int)(row - (long long)tok * P.group)) * P.out.h + c;
   if (P.aligned) {
     if constexpr (sizeof(E) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
@@ -326,15 +363,19 @@ hipError_t launch_seq_token(const SeqParams<bf16_t>& P, hipStream_t st) {
 
 template <typename E>
 hipError_t launch_seq_join(const SeqParams<E>& P, hipStream_t st) {
+  const long long rows = (long long)P.tokens_q * P.group;
+  auto go = [&](auto dc) -> hipError_t {
+    constexpr int D = decltype(dc)::value;
+    const bool many = P.ranges >= 8;
+    const long long per = many ? 256 / (D / 4) / 4 : 256 / (D / 4), blocks = (rows + per - 1) / per;
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)blocks, (unsigned)P.heads_kv);
+    if (many) hipLaunchKernelGGL((seq_join_kernel<E, D, 4>), grid, dim3(256), 0, st, P);
+    else hipLaunchKernelGGL((seq_join_kernel<E, D, 1>), grid, dim3(256), 0, st, P);
+    return hipGetLastError();
+  };
   const int D = seq_padded(P.d);
-  const long long rows = (long long)P.tokens_q * P.group, per = 1024 / D;
-  const long long blocks = (rows + per - 1) / per;
-  if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)blocks, (unsigned)P.heads_kv);
-  if (D == 64) hipLaunchKernelGGL((seq_join_kernel<E, 64>), grid, dim3(256), 0, st, P);
-  else if (D == 128) hipLaunchKernelGGL((seq_join_kernel<E, 128>), grid, dim3(256), 0, st, P);
-  else hipLaunchKernelGGL((seq_join_kernel<E, 256>), grid, dim3(256), 0, st, P);
-  return hipGetLastError();
+  return D == 64 ? go(std::integral_constant<int, 64>{}) : D == 128 ? go(std::integral_constant<int, 128>{}) : go(std::integral_constant<int, 256>{});
 }
 
 template hipError_t launch_seq_token<64>(const SeqParams<bf16_t>&, hipStream_t);
