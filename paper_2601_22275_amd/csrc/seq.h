@@ -89,6 +89,49 @@ __device__ __forceinline__ Span find_tile(const int* starts, int n_seqs, int tok
   return w;
 }
 
+// The same tiles in order of their work under a causal mask, most first, for up to 64 sequences: with n_s tiles in sequence s, tile r - 1 sees (as
+// queries; as keys, tile n_s - r is seen by) r tiles' worth, so the order is by r, all sequences together.  Above r lie G(r) = sum_s max(n_s - r, 0)
+// tiles.  Sequences one after another leave the card waiting for the last long one (3 x 4096 tokens, 12 heads on 4, d = 128, forward and backward:
+// 730 -> 692 us; 7 prompts of up to 5000 346 -> 304).  `tile` is r - 1 here.
+__device__ __forceinline__ Span find_tile_by_work(const int* starts, int n_seqs, int tokens, int rows_per_token, int BM, int t) {
+  const int lane = threadIdx.x & 63;
+  int begin = 0, count = 0;
+  if (lane < n_seqs) {
+    begin = start_of(starts, lane, tokens);
+    count = max(start_of(starts, lane + 1, tokens) - begin, 0);
+  }
+  const int n = (int)(((long long)count * rows_per_token + BM - 1) / BM);
+  auto above = [&](int r) {
+    int x = max(n - r, 0);
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) x += __shfl_xor(x, step);
+    return __builtin_amdgcn_readfirstlane(x);
+  };
+  Span w = {0, 0, 0, 0};
+  int most = n;
+#pragma unroll
+  for (int step = 1; step < 64; step *= 2) most = max(most, __shfl_xor(most, step));
+  most = __builtin_amdgcn_readfirstlane(most);
+  if (t >= above(0)) return w;
+  int lo = 0, hi = most;  // G(lo) > t >= G(hi)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (above(mid) > t) lo = mid;
+    else hi = mid;
+  }
+  const int nth = t - above(hi);
+  const unsigned long long have = __ballot(n >= hi);
+  // the sequence with `nth` others of as many tiles in front of it
+  const bool here = n >= hi && __builtin_popcountll(have & ((1ull << lane) - 1)) == nth;
+  w.seq = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(__ballot(here)));
+  w.begin = __shfl(begin, w.seq);
+  w.count = __shfl(count, w.seq);
+  w.begin = __builtin_amdgcn_readfirstlane(w.begin);
+  w.count = __builtin_amdgcn_readfirstlane(w.count);
+  w.tile = hi - 1;
+  return w;
+}
+
 // Upper bound of the tiles of all sequences (see find_tile)
 inline long long tile_bound(long long tokens, int rows_per_token, int BM, int n_seqs) { return tokens * rows_per_token / BM + n_seqs; }
 

@@ -66,7 +66,12 @@ __global__ void __launch_bounds__(64 * waves<MODE>(), 2) seq_bwd_kernel(SeqParam
   const int kvh = blockIdx.x % P.heads_kv;
   const int tiles = gridDim.x / P.heads_kv, at = blockIdx.x / P.heads_kv;
   // under a causal mask the last queries see most keys, and the first keys are seen by most queries: those start first
-  const Span w = MODE == DKV ? find_tile(P.k_starts, P.n_seqs, P.tokens_k, 1, BO, at) : find_tile(P.q_starts, P.n_seqs, P.tokens_q, P.group, BO, tiles - 1 - at);
+  const bool by_work = P.causal && P.n_seqs <= 64;
+  const int* own_starts = MODE == DKV ? P.k_starts : P.q_starts;
+  const int own_tokens = MODE == DKV ? P.tokens_k : P.tokens_q, per_token = MODE == DKV ? 1 : P.group;
+  Span w = by_work ? find_tile_by_work(own_starts, P.n_seqs, own_tokens, per_token, BO, at)
+                   : find_tile(own_starts, P.n_seqs, own_tokens, per_token, BO, MODE == DKV ? at : tiles - 1 - at);
+  if (MODE == DKV && by_work) w.tile = max((w.count + BO - 1) / BO - 1 - w.tile, 0);
   int q_begin, nq, k_begin, nk;
   if (MODE == DKV) {
     k_begin = w.begin;

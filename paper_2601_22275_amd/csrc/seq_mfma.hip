@@ -66,8 +66,9 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
   // Workgroups with neighbouring numbers go to different XCDs; heads innermost, so that an XCD's share repeats few heads and keeps their
   // keys in its L2.  Later tiles first: under a causal mask they see more keys.
   const int kvh = blockIdx.x % P.heads_kv;
-  const int tiles = gridDim.x / P.heads_kv;
-  const Span w = find_tile(P.q_starts, P.n_seqs, P.tokens_q, P.group, BQ, tiles - 1 - blockIdx.x / P.heads_kv);
+  const int tiles = gridDim.x / P.heads_kv, nth = blockIdx.x / P.heads_kv;
+  const Span w = P.causal && P.n_seqs <= 64 ? find_tile_by_work(P.q_starts, P.n_seqs, P.tokens_q, P.group, BQ, nth)
+                                            : find_tile(P.q_starts, P.n_seqs, P.tokens_q, P.group, BQ, tiles - 1 - nth);
   const long long rows = (long long)w.count * P.group;
   const long long row_first = (long long)w.tile * BQ;
   if (row_first >= rows) return;
