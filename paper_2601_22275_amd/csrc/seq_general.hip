@@ -1,7 +1,8 @@
 // Attention over packed sequences and over pages, forward and backward, on the fp32 matrix units of gfx950: any d <= 256, any strides,
 // float32 or bf16 in memory.  What the bf16 kernels (seq_mfma.hip, seq_bwd.hip) do not take runs here, float32 among it.
 //
-// A workgroup is four waves of 16 owner rows; the other tensor's rows stream through LDS in tiles of 32, in fp32.  All products are
+// A workgroup is four waves of 16 owner rows, or twice four that take every other tile of the stream and add up at the end (one chain of work
+// half as long); the other tensor's rows stream through LDS in tiles of 32, in fp32.  All products are
 // v_mfma_f32_16x16x4_f32, in the form X^T = (stream rows) (owner rows)^T, so that lane (i = lane % 16, g = lane / 16) holds owner row i
 // and stream rows 4 g .. + 3 of a block of 16: a softmax row's sums are per-lane scalars plus one exchange among four lanes, and
 // the weights are the B operand of the next product as they stand (its k index runs over rows 4 g + r for fixed r).  The order of the
@@ -60,6 +61,16 @@ __device__ __forceinline__ void store4(E* row, int c, int d, bool aligned, float
   if (c + 3 < d) store_f<E>(row + c + 3, f3);
 }
 
+// Maximum over the four lanes of an owner row (lane % 16 alike), without a trip through LDS
+__device__ __forceinline__ float across_max(float x) {
+  unsigned u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  u = __float_as_uint(x);
+  const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 template <typename E>
 __device__ __forceinline__ const E* key_row(const SeqParams<E>& P, const KeyRows<E>& K, int seq, int begin, int kvh, int j) {
   if (P.page_size == 0) return K.p + (long long)(begin + j) * K.t + kvh * K.h;
@@ -71,23 +82,36 @@ __device__ __forceinline__ const E* key_row(const SeqParams<E>& P, const KeyRows
 
 enum { FORWARD = 0, GRAD_Q = 1, GRAD_KV = 2 };
 
+// Halves of a workgroup (a wave of d = 256 needs more registers than eight waves have each)
+template <int D>
+constexpr int parts() {
+  return D == 256 ? 1 : 2;
+}
+
 template <typename E, int D, int MODE>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqParams<E> P) {
+__global__ void __launch_bounds__(256 * parts<D>(), D == 256 ? 1 : 2) seq_general_kernel(SeqParams<E> P) {
   constexpr int LS = D + 4;          // floats of an LDS row: 16 rows of four channels fall on all banks
   constexpr int NJ = D / 16;         // 16-channel groups of a contraction over channels
   constexpr int NC = D / 64;         // 64-channel groups of an output row
   constexpr bool BWD = MODE != FORWARD;
-  __shared__ __attribute__((aligned(16))) float x1[BN][LS];  // keys (GRAD_KV: queries)
-  __shared__ __attribute__((aligned(16))) float x2[BN][LS];  // values (GRAD_KV: d_out)
-  __shared__ float st_lse[MODE == GRAD_KV ? BN : 1], st_delta[MODE == GRAD_KV ? BN : 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, g = lane >> 4;
+  constexpr int PARTS = parts<D>();
+  __shared__ __attribute__((aligned(16))) float tiles_lds[PARTS][2][BN][LS];
+  __shared__ float st_lds[PARTS][2][MODE == GRAD_KV ? BN : 1];
+  const int part = threadIdx.x / 256, tid = threadIdx.x % 256;
+  float (&x1)[BN][LS] = tiles_lds[part][0];  // keys (GRAD_KV: queries)
+  float (&x2)[BN][LS] = tiles_lds[part][1];  // values (GRAD_KV: d_out)
+  float (&st_lse)[MODE == GRAD_KV ? BN : 1] = st_lds[part][0], (&st_delta)[MODE == GRAD_KV ? BN : 1] = st_lds[part][1];
+  const int lane = tid & 63, wave = tid >> 6, li = lane & 15, g = lane >> 4;
   const int kvh = blockIdx.y;
   const int group = P.group, d = P.d;
   const bool al = P.aligned;
 
-  const int tiles = gridDim.x;
-  const int t = tiles - 1 - blockIdx.x;  // causal: later tiles see more keys and start first
-  const Span w = MODE == GRAD_KV ? find_tile(P.k_starts, P.n_seqs, P.tokens_k, 1, BM, t) : find_tile(P.q_starts, P.n_seqs, P.tokens_q, group, BM, t);
+  const int* own_starts = MODE == GRAD_KV ? P.k_starts : P.q_starts;
+  const int own_tokens = MODE == GRAD_KV ? P.tokens_k : P.tokens_q, per_token = MODE == GRAD_KV ? 1 : group;
+  const bool by_work = P.causal && P.n_seqs <= 64;
+  Span w = by_work ? find_tile_by_work(own_starts, P.n_seqs, own_tokens, per_token, BM, blockIdx.x)
+                   : find_tile(own_starts, P.n_seqs, own_tokens, per_token, BM, gridDim.x - 1 - blockIdx.x);
+  if (MODE == GRAD_KV && by_work) w.tile = max((w.count + BM - 1) / BM - 1 - w.tile, 0);
   int q_begin, nq, k_begin, nk;
   if (MODE == GRAD_KV) {
     k_begin = w.begin;
@@ -173,7 +197,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
   auto fetch = [&](int tile) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int piece = i * 256 + threadIdx.x;
+      const int piece = i * 256 + tid;
       const long long r = s0 + (long long)tile * BN + piece / (D / 4);
       const int c = piece % (D / 4) * 4;
       if (r < s1) {
@@ -204,13 +228,14 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
   for (int round = exact ? 0 : 1; round < 2; ++round) {
   if (MODE == GRAD_Q && exact && round == 0) o_delta = 0.f;
   float d_sum = 0.f;
-  if (ntiles > 0) fetch(0);
-  for (int tile = 0; tile < ntiles; ++tile) {
+  // (past the last tile the half that has none left multiplies zeros)
+  if (ntiles > 0) fetch(part);
+  for (int tile = part; tile - part < ntiles; tile += PARTS) {
     const long long base = s0 + (long long)tile * BN;
     bool odd_value = false;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int piece = i * 256 + threadIdx.x;
+      const int piece = i * 256 + tid;
       const int r = piece / (D / 4), c = piece % (D / 4) * 4;
       *reinterpret_cast<f32x4*>(&x1[r][c]) = f1[i];
       *reinterpret_cast<f32x4*>(&x2[r][c]) = f2[i];
@@ -219,8 +244,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
         for (int e = 0; e < 4; ++e) odd_value = odd_value || !(fabsf(f2[i][e]) < INFINITY);
       }
     }
-    if (MODE == GRAD_KV && threadIdx.x < BN) {
-      const long long r = base + threadIdx.x;
+    if (MODE == GRAD_KV && tid < BN) {
+      const long long r = base + tid;
       float a = INFINITY, b = 0.f;
       if (r < s1) {
         const long long at = stat_of(r);
@@ -228,13 +253,13 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
         b = P.delta[at];
         if (a == -INFINITY) a = INFINITY;
       }
-      st_lse[threadIdx.x] = a;
-      st_delta[threadIdx.x] = b;
+      st_lse[MODE == GRAD_KV ? tid : 0] = a;
+      st_delta[MODE == GRAD_KV ? tid : 0] = b;
     }
     // a value that is not finite takes the slow way below where not all rows see all keys of the tile
     if (MODE == FORWARD) odd_value = __syncthreads_or(odd_value) != 0;
     else __syncthreads();
-    if (tile + 1 < ntiles) fetch(tile + 1);
+    if (tile + PARTS - part < ntiles) fetch(tile + PARTS);
 
     f32x4 s[2], dp[2];
 #pragma unroll
@@ -266,8 +291,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
           s[kb][r] = v ? s[kb][r] * sc : -INFINITY;
           top = fmaxf(top, s[kb][r]);
         }
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
+      top = across_max(top);
       const float m2 = fmaxf(m, top);
       const float ref = m2 == -INFINITY ? 0.f : m2;
       const float alpha = __builtin_amdgcn_exp2f(m - ref);
@@ -297,8 +321,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
           } else {
             const long long row = base + sr;
             v = ovalid && row < s1 && (!P.causal || orow <= (long long)more + row / group);
-            lse2 = st_lse[sr];
-            delta = st_delta[sr];
+            lse2 = st_lse[MODE == GRAD_KV ? sr : 0];
+            delta = st_delta[MODE == GRAD_KV ? sr : 0];
           }
           p[kb][r] = v ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][r], sc, -lse2)) : 0.f;
           ds[kb][r] = v ? p[kb][r] * (dp[kb][r] - delta) : 0.f;
@@ -369,12 +393,46 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) seq_general_kernel(SeqP
   if (MODE == GRAD_Q && round == 0) {
     d_sum += __shfl_xor(d_sum, 16);
     d_sum += __shfl_xor(d_sum, 32);
+    if (PARTS == 2) {  // both halves' sums
+      float* buf = &tiles_lds[0][0][0][0];
+      buf[threadIdx.x] = d_sum;
+      __syncthreads();
+      d_sum += buf[threadIdx.x ^ 256];
+      __syncthreads();
+    }
     o_delta = d_sum;
   }
   }
-  if (MODE == GRAD_Q && ovalid && g == 0) P.delta[stat_of(orow)] = o_delta;
+  if (MODE == GRAD_Q && ovalid && g == 0 && part == 0) P.delta[stat_of(orow)] = o_delta;
 
   // ---- epilogue -----------------------------------------------------------------------------------------------------------------
+  if (PARTS == 2) {
+    // the second half hands over what it has (every wave is past the last barrier of the stream: the tiles are free)
+    float* buf = &tiles_lds[0][0][0][0];
+    constexpr int REGS = NACC * NC * 16;
+    static_assert(PARTS == 1 || (REGS + 2) * 256 <= PARTS * 2 * BN * LS, "a half's sums fit the tiles");
+    if (part == 1) {
+#pragma unroll
+      for (int i = 0; i < REGS; ++i) buf[i * 256 + tid] = acc[i / (NC * 16)][i / 16 % NC][i / 4 % 4][i % 4];
+      buf[REGS * 256 + tid] = m;
+      buf[(REGS + 1) * 256 + tid] = l;
+    }
+    __syncthreads();
+    if (part == 1) return;
+    float a0 = 1.f, a1 = 1.f;
+    if (MODE == FORWARD) {
+      const float m1 = buf[REGS * 256 + tid], m2 = fmaxf(m, m1), ref = m2 == -INFINITY ? 0.f : m2;
+      a0 = __builtin_amdgcn_exp2f(m - ref);
+      a1 = __builtin_amdgcn_exp2f(m1 - ref);
+      l = l * a0 + buf[(REGS + 1) * 256 + tid] * a1;
+      m = m2;
+    }
+#pragma unroll
+    for (int i = 0; i < REGS; ++i) {
+      f32x4& x = acc[i / (NC * 16)][i / 16 % NC][i / 4 % 4];
+      x[i % 4] = MODE == FORWARD ? x[i % 4] * a0 + buf[i * 256 + tid] * a1 : x[i % 4] + buf[i * 256 + tid];
+    }
+  }
   float f = P.scale;
   if (MODE == FORWARD) {
     l += __shfl_xor(l, 16);
@@ -416,8 +474,8 @@ hipError_t launch(const SeqParams<E>& P, hipStream_t st) {
   const long long tiles = MODE == GRAD_KV ? tile_bound(P.tokens_k, 1, BM, P.n_seqs) : tile_bound(P.tokens_q, P.group, BM, P.n_seqs);
   if (tiles > 0x7fffffffLL) return hipErrorInvalidValue;
   const dim3 grid((unsigned)tiles, (unsigned)P.heads_kv, (unsigned)(MODE == FORWARD && P.ranges > 1 ? P.ranges : 1));
-  if (P.d <= 64) hipLaunchKernelGGL((seq_general_kernel<E, 64, MODE>), grid, dim3(256), 0, st, P);
-  else if (P.d <= 128) hipLaunchKernelGGL((seq_general_kernel<E, 128, MODE>), grid, dim3(256), 0, st, P);
+  if (P.d <= 64) hipLaunchKernelGGL((seq_general_kernel<E, 64, MODE>), grid, dim3(512), 0, st, P);
+  else if (P.d <= 128) hipLaunchKernelGGL((seq_general_kernel<E, 128, MODE>), grid, dim3(512), 0, st, P);
   else hipLaunchKernelGGL((seq_general_kernel<E, 256, MODE>), grid, dim3(256), 0, st, P);
   return hipGetLastError();
 }

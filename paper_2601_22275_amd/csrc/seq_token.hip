@@ -7,7 +7,8 @@
 // barrier in the loop, a wave waits for its own loads only; two workgroups share a compute unit, so that one's start and end pass behind the
 // other's stream.  The waves join through LDS at the end, the ranges (blockIdx.y) through memory and a second launch.
 // 16 single tokens over up to 16,384 keys, 40 heads on 8, d = 128 (585 MB): 136 us, 4.3 TB/s with the join, where a large copy moves 5.0;
-// four waves in one workgroup 142, every lane forming the addresses of the rows it loads 160.  Products as in seq_mfma.hip: S^T = K Q^T and O^T += V^T P^T, both
+// four waves in one workgroup 142, every lane forming the addresses of the rows it loads 160.  d = 64, 40 heads on 10 (366 MB): 90 us,
+// 4.1 TB/s; with four sub-tiles in LDS and two workgroups on a unit 110.  Products as in seq_mfma.hip: S^T = K Q^T and O^T += V^T P^T, both
 // v_mfma_f32_32x32x16_bf16.
 #include "seq_device.h"
 
@@ -17,17 +18,12 @@ namespace {
 
 constexpr int NW = 2;
 
-// Sub-tiles in flight per wave: 128 KB of LDS either way
-template <int D>
-constexpr int slots() {
-  return D == 128 ? 2 : 4;
-}
+constexpr int NS = 2;  // sub-tiles in LDS per wave: 64 KB a workgroup at d = 128, half that at d = 64 (two and three workgroups on a unit)
 
 template <int D>
-__global__ void __launch_bounds__(64 * NW, 2) seq_token_kernel(SeqParams<bf16_t> P) {
+__global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) seq_token_kernel(SeqParams<bf16_t> P) {
   using G = RowGeo<D>;
   constexpr int ROW_BYTES = G::ROW_BYTES, KS = G::KS, CT = G::CT, CH = G::CH, RPI = G::RPI;
-  constexpr int NS = slots<D>();
   constexpr int SUB_BYTES = 32 * ROW_BYTES;
   constexpr int NR = 32 / RPI;               // loads of a tensor per sub-tile
   constexpr int SLOT_BYTES = 2 * SUB_BYTES;  // keys, then values
@@ -159,13 +155,9 @@ __global__ void __launch_bounds__(64 * NW, 2) seq_token_kernel(SeqParams<bf16_t>
 
 #pragma unroll 1
   for (int i = 0; i < mine; ++i) {
-    // this sub-tile's loads have arrived when no more than those of the sub-tiles behind it are under way
+    // this sub-tile's loads have arrived when no more than those of the one behind it are under way
     constexpr int LOADS = 2 * NR + 1;
-    static_assert((NS - 1) * LOADS < 64, "the counter holds what is in flight");
-    const int behind = min(mine - 1 - i, NS - 1);
-    if (NS == 4 && behind == 3) asm volatile("s_waitcnt vmcnt(%0)" : : "n"((NS - 1) * LOADS) : "memory");
-    else if (NS == 4 && behind == 2) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * LOADS) : "memory");
-    else if (behind >= 1) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(LOADS) : "memory");
+    if (i + 1 < mine) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(LOADS) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (i + NS < mine) prepare(i + NS);  // (its pages came in front of this sub-tile's rows)
     const unsigned off = (i % NS) * SLOT_BYTES;
@@ -352,7 +344,7 @@ __global__ void __launch_bounds__(256) seq_join_kernel(SeqParams<E> P) {
 
 template <int D>
 hipError_t launch_seq_token(const SeqParams<bf16_t>& P, hipStream_t st) {
-  constexpr int LDS = NW * slots<D>() * 2 * 32 * D * 2;
+  constexpr int LDS = NW * NS * 2 * 32 * D * 2;
   const long long blocks = tile_bound(P.tokens_q, P.group, 32, P.n_seqs) * P.heads_kv;
   if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
   static const hipError_t configured = hipFuncSetAttribute((const void*)seq_token_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
