@@ -330,27 +330,32 @@ __global__ void __launch_bounds__(64 * waves<MODE>(), 2) seq_bwd_kernel(SeqParam
       }
     }
     bf16x8 pb[2], eb[2];  // P, dS
-#pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      f32x4 l2 = {o_l2, o_l2, o_l2, o_l2}, dd = {o_delta, o_delta, o_delta, o_delta};
+    f32x4 l2 = {o_l2, o_l2, o_l2, o_l2}, dd = {o_delta, o_delta, o_delta, o_delta};
+    auto stats = [&](auto r4_c) __attribute__((always_inline)) {  // of stream rows 8 r4 + 4 g .. + 3
       if (MODE == DKV) {
-        const unsigned sa = sslot + (32 * ST + 8 * r4) * 4;
+        const unsigned sa = sslot + (32 * ST + 8 * decltype(r4_c)::value) * 4;
         l2 = rd_stat(sa);
         dd = rd_stat(sa + SR * 4);
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = 4 * r4 + i;
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc2, -l2[i]));
-        if (SUM) {
-          d_sum = __builtin_fmaf(p, dp[r], d_sum);
-        } else {
-          if (MODE == DKV) pb[r >> 3][r & 7] = (__bf16)p;
-          eb[r >> 3][r & 7] = (__bf16)(p * (dp[r] - dd[i]));
-        }
+    };
+    auto score = [&](auto rc) __attribute__((always_inline)) {
+      constexpr int r = decltype(rc)::value;
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc2, -l2[r & 3]));
+      if (SUM) {
+        d_sum = __builtin_fmaf(p, dp[r], d_sum);
+      } else {
+        if (MODE == DKV) pb[r >> 3][r & 7] = (__bf16)p;
+        eb[r >> 3][r & 7] = (__bf16)(p * (dp[r] - dd[r & 3]));
       }
+    };
+    // The first 16 rows' scores, then the other 16's between the products of the first
+    constexpr int FIRST = SUM ? 4 : 2;
+    static_for<0, FIRST>([&](auto r4_c) __attribute__((always_inline)) {
+      constexpr int r4 = decltype(r4_c)::value;
+      stats(r4_c);
+      static_for<4 * r4, 4 * r4 + 4>(score);
       if (TIGHT) __builtin_amdgcn_sched_barrier(0);
-    }
+    });
     __builtin_amdgcn_sched_barrier(0);
     static_for<NG, LAST>([&](auto ic) __attribute__((always_inline)) {
       constexpr int I = decltype(ic)::value;
@@ -358,6 +363,13 @@ __global__ void __launch_bounds__(64 * waves<MODE>(), 2) seq_bwd_kernel(SeqParam
       request(std::integral_constant<int, I + PF>{});
       if constexpr (x == 1) acc[x][ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[I & 3], pb[c], acc[x][ct], 0, 0, 0);
       else acc[x][ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[I & 3], eb[c], acc[0][ct], 0, 0, 0);
+      if constexpr (c == 0) {
+        constexpr int PER = 8 / (CT * NACC), r0 = 8 + PER * (I - NG);
+        static_for<r0, r0 + PER>([&](auto rc) __attribute__((always_inline)) {
+          if constexpr (decltype(rc)::value % 4 == 0) stats(std::integral_constant<int, decltype(rc)::value / 4>{});
+          score(rc);
+        });
+      }
       __builtin_amdgcn_sched_barrier(0);
     });
   };
