@@ -27,19 +27,37 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(RotaryParams P, RotaryT
   const int t_local = threadIdx.x / units;
   const int unit = threadIdx.x - t_local * units;
   const long long token = (long long)blockIdx.x * tokens_per_block + t_local;
+  int lo = 0, begin = 0, end = 0;  // append: the token's sequence, the last that begins at or before it
+  if (APPEND) {
+    const int n = P.n_seqs;
+    const int tok = (int)min(token, (long long)P.tokens - 1);
+    if (n < 64) {  // the wave holds all starts
+      const int lane = threadIdx.x & 63;
+      const int mine = P.starts[min(lane, n)];
+#pragma unroll
+      for (int step = 32; step > 0; step /= 2) {
+        const int at = __shfl(mine, min(lo + step, 63));
+        if (lo + step < n && at <= tok) lo += step;
+      }
+      begin = __shfl(mine, lo);
+      end = __shfl(mine, lo + 1);
+    } else {
+      int hi = n;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (P.starts[mid] <= tok) lo = mid;
+        else hi = mid;
+      }
+      begin = P.starts[lo];
+      end = P.starts[lo + 1];
+    }
+    end = min(end, P.tokens);
+  }
   if (t_local >= tokens_per_block || token >= P.tokens) return;
 
   long long slot_off[2] = {0, 0};  // append: where the token's slot lies in the caches of keys and of values
   int at = 0;
   if (APPEND) {
-    const int n = P.n_seqs;
-    int lo = 0, hi = n;  // the last sequence that begins at or before the token
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (P.starts[mid] <= token) lo = mid;
-      else hi = mid;
-    }
-    const int begin = P.starts[lo], end = min(P.starts[lo + 1], P.tokens);
     if (token < begin || token >= end) return;
     const long long room = (long long)P.table_width * P.page_size;
     const long long have = min((long long)max(P.lengths[lo], 0), room);
@@ -54,8 +72,8 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(RotaryParams P, RotaryT
   }
 
   const int pairs = P.turned[which];
-  const int turning = HALF ? pairs / V : 2 * pairs / V;  // units with turned pairs (V = 1, interleaved: a unit is a pair)
-  const int turning_units = V == 1 ? pairs : turning;
+  // units with turned pairs (V = 1, interleaved: a unit is a pair; wide: the last may hold pairs that are not turned)
+  const int turning_units = HALF ? pairs / V : V == 1 ? pairs : (2 * pairs + V - 1) / V;
   const bool turns = unit < turning_units;
   int c0, c1 = 0;  // channels of the unit's pieces
   constexpr int NP = V == 1 ? 1 : HALF ? V : V / 2;  // pairs of a unit
@@ -66,7 +84,7 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(RotaryParams P, RotaryT
     const int first = HALF ? unit * V : V == 1 ? unit : unit * (V / 2);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int pair = first + i;
+      const int pair = min(first + i, pairs - 1);
       const int axis = (pair >= P.axis_end[0]) + (pair >= P.axis_end[1]);
       const int pos = P.positions ? P.positions[axis * P.axis_stride + token] : at;
       const double turn = (double)pos * F.per_position[pair];
@@ -77,7 +95,7 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(RotaryParams P, RotaryT
       sn[i] = P.amplitude * P.sign * s;
     }
   } else {
-    c0 = 2 * pairs + (unit - turning_units) * V;
+    c0 = (HALF || V == 1 ? 2 * pairs : turning_units * V) + (unit - turning_units) * V;
     if (c0 >= P.d) return;  // (keys and values of one launch need not have as many units)
   }
 
@@ -120,6 +138,7 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(RotaryParams P, RotaryT
         } else {
 #pragma unroll
           for (int j = 0; j < V / 2; ++j) {
+            if (c0 / 2 + j >= pairs) break;  // the rest of a piece passes through
             const float x0 = load_f<E>(&a[i].e[2 * j]), x1 = load_f<E>(&a[i].e[(2 * j + 1) % V]);
             store_f<E>(&a[i].e[2 * j], x0 * cs[j] - x1 * sn[j]);
             store_f<E>(&a[i].e[(2 * j + 1) % V], x0 * sn[j] + x1 * cs[j]);
@@ -138,7 +157,8 @@ hipError_t launch(const RotaryParams& P, const RotaryTurns& F, hipStream_t st) {
   int units = 0;
   for (int x = 0; x < (append ? 2 : 1); ++x) {
     const int n = P.turned[x];
-    const int u = (V == 1 ? n : half ? n / V : 2 * n / V) + (P.d - 2 * n) / V;
+    const int turning = half ? n / V : V == 1 ? n : (2 * n + V - 1) / V;
+    const int u = turning + (P.d - (half || V == 1 ? 2 * n : turning * V)) / V;
     if (u > units) units = u;
   }
   const int tokens_per_block = THREADS / units;

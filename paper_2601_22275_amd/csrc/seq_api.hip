@@ -120,10 +120,11 @@ void plan_params(const vmonarch_rotary_plan* p, int pairs, RotaryParams* P, Rota
   P->axis_end[2] = pairs;
 }
 
-// Whether the pieces of `elem`-byte channels a thread handles can be 16 bytes: no pair's partner in the middle of another's piece
+// Whether the pieces of `elem`-byte channels a thread handles can be 16 bytes: a pair's partner lies in the same piece (interleaved) or at the same
+// place of another (half, pairs a multiple of a piece)
 bool wide_pieces(int interleaved, int pairs, int d, size_t elem) {
   const int v = 16 / (int)elem;
-  return d % v == 0 && (interleaved ? 2 * pairs : pairs) % v == 0;
+  return d % v == 0 && (interleaved || pairs % v == 0);
 }
 
 int rotary_impl(const vmonarch_tokens* q, const vmonarch_tokens* q_out, int heads_q, const vmonarch_tokens* k, const vmonarch_tokens* k_out, int heads_k,
