@@ -37,17 +37,11 @@ constexpr float MOVE_ALONG2 = 8.0f;   // rows of the wave this far above their r
 // issue slots were measured short (the last register of the last accumulator, copied right behind them, was old); these are twenty.
 #define SQ_MFMA_RESULT_WAIT() asm volatile("s_nop 15\n\ts_nop 3" ::: "memory")
 
-// Key rows of an LDS tile: two workgroups share a compute unit at 32 rows and d = 128
-template <int D>
-constexpr int tile_rows() {
-  return D == 128 ? 32 : 64;
-}
-
-template <int D, bool PAGED, bool SPLIT, bool STAT>
+// BT: key rows of an LDS tile.  32: two workgroups share a compute unit at d = 128, three at d = 64; 64 (d = 64): two, and half the barriers.
+template <int D, int BT, bool PAGED, bool SPLIT, bool STAT>
 __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf16_t> P) {
   using G = RowGeo<D>;
   constexpr int ROW_BYTES = G::ROW_BYTES;
-  constexpr int BT = tile_rows<D>();
   constexpr int TILE_BYTES = BT * ROW_BYTES;
   constexpr int KS = G::KS, CT = G::CT, CH = G::CH, RPI = G::RPI;
   constexpr int V_OFF = NSLOT * TILE_BYTES;
@@ -566,12 +560,12 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
   }
 }
 
-template <int D, bool PAGED, bool SPLIT, bool STAT>
+template <int D, int BT, bool PAGED, bool SPLIT, bool STAT>
 hipError_t launch(const SeqParams<bf16_t>& P, hipStream_t st) {
-  constexpr int LDS = 2 * NSLOT * tile_rows<D>() * D * 2;
+  constexpr int LDS = 2 * NSLOT * BT * D * 2;
   const long long blocks = tile_bound(P.tokens_q, P.group, 32 * W2, P.n_seqs) * P.heads_kv;
   if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-  auto kern = seq_attention_kernel<D, PAGED, SPLIT, STAT>;
+  auto kern = seq_attention_kernel<D, BT, PAGED, SPLIT, STAT>;
   static const hipError_t configured = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (configured != hipSuccess) return configured;
   hipLaunchKernelGGL(kern, dim3((unsigned)blocks, (unsigned)(SPLIT ? P.ranges : 1)), dim3(64 * W2), LDS, st, P);
@@ -585,8 +579,23 @@ hipError_t launch(const SeqParams<bf16_t>& P, hipStream_t st) {
 
 template <int D>
 hipError_t launch_seq_attention_mfma(const SeqParams<bf16_t>& P, hipStream_t st) {
-  if (P.page_size > 0) return P.ranges > 1 ? launch<D, true, true, false>(P, st) : launch<D, true, false, false>(P, st);
-  return P.lse != nullptr ? launch<D, false, false, true>(P, st) : launch<D, false, false, false>(P, st);
+  auto run = [&](auto bt) -> hipError_t {
+    constexpr int BT = decltype(bt)::value;
+    if (P.page_size > 0) return launch<D, BT, true, false, false>(P, st);
+    return P.lse != nullptr ? launch<D, BT, false, false, true>(P, st) : launch<D, BT, false, false, false>(P, st);
+  };
+  using rows32 = std::integral_constant<int, 32>;
+  using rows64 = std::integral_constant<int, 64>;
+  if constexpr (D == 64) {
+    // Tiles of 64 keys while two workgroups a unit take the whole launch, tiles of 32 and three of them beyond (64 / 32, us: a dozen prompts of up to 700
+    // tokens, 12 heads on 4, 440 workgroups 20.9 / 23.9; 4 clips on 512 keys, 10 heads, 670 23.3 / 20.3; 16,384 causal tokens, 12 heads, 1536 485 /
+    // 453, 8192 without a mask 271 / 224).
+    if (P.page_size > 0 && P.ranges > 1) return launch<D, 64, true, true, false>(P, st);
+    return tile_bound(P.tokens_q, P.group, 32 * W2, P.n_seqs) * P.heads_kv > 2LL * compute_units() ? run(rows32{}) : run(rows64{});
+  } else {
+    if (P.page_size > 0 && P.ranges > 1) return launch<D, 32, true, true, false>(P, st);
+    return run(rows32{});
+  }
 }
 
 // This file is compiled once per head dimension.

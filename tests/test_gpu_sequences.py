@@ -430,3 +430,30 @@ def test_binding_refusals(B):
         with pytest.raises(B.VMonarchError):
             f()
             print("accepted:", i)
+
+
+@pytest.mark.parametrize("d,kv,group,n,causal", [(64, 12, 1, 5700, True), (64, 6, 2, 5700, False), (128, 12, 1, 5700, True), (64, 2, 1, 2100, False)])
+def test_launches_of_many_workgroups(B, d, kv, group, n, causal):
+    """More workgroups than run at once (other tiles at d = 64), keys packed and in pages; a few rows of every head are compared."""
+    gen = torch.Generator().manual_seed(n + d)
+    lens = [n, n // 3 + 1]
+    heads = kv * group
+    q, k, v = tokens(gen, sum(lens), heads, d, "bf16", "token", 1.5), tokens(gen, sum(lens), kv, d, "bf16", "token", 1.3), tokens(gen, sum(lens), kv, d, "bf16")
+    s, have = starts(lens), torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out, lse = B.packed_attention(q, k, v, s, causal=causal, lse=True)
+    assert torch.equal(out, B.packed_attention(q, k, v, s, causal=causal))
+    ck, cv, table = pages(gen, lens, 100, kv, d, "bf16")
+    B.paged_append(k, v, ck, cv, table, s, have)
+    paged = B.paged_attention(q, ck, cv, table, s, have, causal=causal)
+    scale = float(np.float32(1.0 / math.sqrt(d)))
+    kc, vc = f64(k), f64(v)
+    for a, m in zip((0, n), lens):
+        rows = np.unique([0, 31, 127, 128, m // 2, m - 1])
+        for h in range(heads):
+            g = h // group
+            for i in rows:
+                seen = i + 1 if causal else m
+                r = S.attention(f64(q[a + i:a + i + 1, h]), kc[a:a + seen, g], vc[a:a + seen, g], scale, False, "bf16")
+                for name, got in (("out", out[a + i, h]), ("out", paged[a + i, h]), ("lse", lse[h, a + i])):
+                    ref, bound = r[name]
+                    assert (np.abs(f64(got) - ref[0]) <= bound[0]).all(), (name, h, i)
