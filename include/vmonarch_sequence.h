@@ -17,8 +17,9 @@
  *   - causal != 0: query i of a sequence's nq sees its keys 0 .. nk - nq + i; causal == 0: all nk.  A row that sees no
  *     key, or whose logits are all -inf, gives zeros and a log-sum-exp of -inf.  Keys and values that a row does not see do not
  *     reach it, infinities and NaN among them (forward passes; gradients are defined for finite tensors).
- *   - bf16 with d <= 128, d a multiple of 8 and rows on 16-byte boundaries runs on the bf16 matrix units; everything
- *     else on the fp32 matrix units, with the same results to the tensors' precision.
+ *   - bf16 with d <= 128, d a multiple of 8, rows on 16-byte boundaries (and packed keys less than 2^24 elements apart)
+ *     runs on the bf16 matrix units; everything else on the fp32 matrix units, with the same results to the tensors'
+ *     precision.  Values beyond 2^98 may overflow in sums that would not overflow as weights of at most 1.
  *   - Results do not depend on the order in which workgroups run: nothing is accumulated across them by atomics.
  */
 #ifndef VMONARCH_SEQUENCE_H_

@@ -1,6 +1,8 @@
 // Declarations shared by the token-sequence units (rotary.hip, seq_*.hip; not part of the ABI).
 #pragma once
 #include "../../include/vmonarch_sequence.h"
+#include <atomic>
+
 #include "common.h"
 
 namespace vm {
@@ -145,6 +147,18 @@ __device__ __forceinline__ int keys_of(const SeqParams<E>& P, int s, int* begin)
   }
   *begin = start_of(P.k_starts, s, P.tokens_k);
   return max(start_of(P.k_starts, s + 1, P.tokens_k) - *begin, 0);
+}
+
+// Lets a kernel use `bytes` of LDS on the current device; done: which devices have it already
+inline hipError_t allow_lds(const void* kernel, int bytes, std::atomic<unsigned long long>* done) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (dev < 64 && (done->load(std::memory_order_acquire) & bit)) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) done->fetch_or(bit, std::memory_order_release);
+  return e;
 }
 
 // ---- launchers (host) -----------------------------------------------------------------------------------------------------------

@@ -514,7 +514,8 @@ hipError_t launch(const SeqParams<bf16_t>& P, hipStream_t st) {
   const long long tiles = MODE == DKV ? tile_bound(P.tokens_k, 1, 32 * NT, P.n_seqs) : tile_bound(P.tokens_q, P.group, 32 * NT, P.n_seqs);
   if (tiles * P.heads_kv > 0x7fffffffLL) return hipErrorInvalidValue;
   auto kern = seq_bwd_kernel<D, MODE>;
-  static const hipError_t configured = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  static std::atomic<unsigned long long> done{0};
+  const hipError_t configured = allow_lds((const void*)kern, LDS, &done);
   if (configured != hipSuccess) return configured;
   hipLaunchKernelGGL(kern, dim3((unsigned)(tiles * P.heads_kv), (unsigned)(MODE == DKV && P.ranges > 1 ? P.ranges : 1)), dim3(64 * waves<MODE>()), LDS, st, P);
   hipError_t e = hipGetLastError();

@@ -6,7 +6,7 @@
 //   S^T = K Q^T        lane (q, g) holds the logits of query q for 16 of 32 keys: sums of a row are per-lane scalars
 //   O^T += V^T P^T     A = V^T by LDS transpose reads, B = P^T, the S^T accumulator converted to bf16 where it stands
 // p = 2^(s scale log2 e - reference); the reference of a row comes from its first 32 logits and any reference gives the same result (the
-// weights have fp32's exponent range in bf16 too): it moves only when a sub-tile's weights add up to more than 2^32, checked after the
+// weights have fp32's exponent range in bf16 too): it moves only when a sub-tile's weights add up to more than 2^12, checked after the
 // fact (the sub-tile is then formed again).  The accumulators are divided by the sum of the ROUNDED weights, so that a row is an exact convex
 // combination; the log-sum-exp is of the unrounded ones.
 // The keys that all rows of a workgroup see whole go through a software pipeline over 32-key sub-tiles (logits of n + 1, softmax of n,
@@ -26,16 +26,16 @@ namespace {
 
 constexpr int W2 = 4;  // waves per workgroup
 constexpr int NSLOT = 4;
-// Sums of a sub-tile's weights above STEP_LARGE2 move the reference (log2: a row has grown by 2^32 since it was set); the accumulators
-// then have 2^(127 - 32 - 17) left for values at 2^17 keys.
-constexpr float STEP_LARGE2 = 4294967296.0f;
+// Sums of a sub-tile's weights above this move the reference (a row has grown by 2^7 and more since it was set): the accumulators then have room
+// for values up to 2^(127 - 12 - 17) over 2^17 keys.
+constexpr float STEP_LARGE2 = 4096.0f;
 constexpr float HEADROOM2 = 16.0f;    // a reference that moves is put this far above the row's maximum
 constexpr float MOVE_ALONG2 = 8.0f;   // rows of the wave this far above their reference move along
 
 #define SQ_FENCE() __builtin_amdgcn_sched_barrier(0)
 // The hardware does not interlock an MFMA's result against plain vector instructions, and the compiler does not see these MFMAs.  Twelve
-// issue slots were measured short (the last register of the last accumulator, copied right behind them, was old); these are twenty.
-#define SQ_MFMA_RESULT_WAIT() asm volatile("s_nop 15\n\ts_nop 3" ::: "memory")
+// issue slots were measured short (the last register of the last accumulator, copied right behind them, was old); these are twenty-four.
+#define SQ_MFMA_RESULT_WAIT() asm volatile("s_nop 15\n\ts_nop 7" ::: "memory")
 
 // BT: key rows of an LDS tile.  32: two workgroups share a compute unit at d = 128, three at d = 64; 64 (d = 64): two, and half the barriers.
 template <int D, int BT, bool PAGED, bool SPLIT, bool STAT>
@@ -566,7 +566,8 @@ hipError_t launch(const SeqParams<bf16_t>& P, hipStream_t st) {
   const long long blocks = tile_bound(P.tokens_q, P.group, 32 * W2, P.n_seqs) * P.heads_kv;
   if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
   auto kern = seq_attention_kernel<D, BT, PAGED, SPLIT, STAT>;
-  static const hipError_t configured = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  static std::atomic<unsigned long long> done{0};
+  const hipError_t configured = allow_lds((const void*)kern, LDS, &done);
   if (configured != hipSuccess) return configured;
   hipLaunchKernelGGL(kern, dim3((unsigned)blocks, (unsigned)(SPLIT ? P.ranges : 1)), dim3(64 * W2), LDS, st, P);
   return hipGetLastError();

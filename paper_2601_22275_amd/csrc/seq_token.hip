@@ -347,7 +347,8 @@ hipError_t launch_seq_token(const SeqParams<bf16_t>& P, hipStream_t st) {
   constexpr int LDS = NW * NS * 2 * 32 * D * 2;
   const long long blocks = tile_bound(P.tokens_q, P.group, 32, P.n_seqs) * P.heads_kv;
   if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-  static const hipError_t configured = hipFuncSetAttribute((const void*)seq_token_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  static std::atomic<unsigned long long> done{0};
+  const hipError_t configured = allow_lds((const void*)seq_token_kernel<D>, LDS, &done);
   if (configured != hipSuccess) return configured;
   hipLaunchKernelGGL(seq_token_kernel<D>, dim3((unsigned)blocks, (unsigned)P.ranges), dim3(64 * NW), LDS, st, P);
   return hipGetLastError();

@@ -457,3 +457,43 @@ def test_launches_of_many_workgroups(B, d, kv, group, n, causal):
                 for name, got in (("out", out[a + i, h]), ("out", paged[a + i, h]), ("lse", lse[h, a + i])):
                     ref, bound = r[name]
                     assert (np.abs(f64(got) - ref[0]) <= bound[0]).all(), (name, h, i)
+
+
+@pytest.mark.parametrize("dtype,d,page", [("bf16", 64, 16), ("bf16", 128, 7), ("bf16", 33, 4), ("f32", 64, 16)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_more_sequences_than_a_wave_has_lanes(B, dtype, d, page, causal):
+    """150 sequences, some empty on one side, short and of a few tiles; every element, forward, backward and over pages."""
+    rng = np.random.default_rng(d)
+    ql, kl = rng.integers(0, 6, 150), rng.integers(0, 9, 150)
+    ql[[3, 70, 149]], kl[[3, 70, 149]] = [90, 40, 130], [90, 77, 20]
+    gen = torch.Generator().manual_seed(d)
+    q, do = (tokens(gen, int(ql.sum()), 4, d, dtype) for _ in range(2))
+    k, v = (tokens(gen, int(kl.sum()), 2, d, dtype) for _ in range(2))
+    qs, ks = starts(ql), starts(kl)
+    out, lse = B.packed_attention(q, k, v, qs, ks, causal=causal, lse=True)
+    want = S.packed(f64(q), f64(k), f64(v), qs.tolist(), ks.tolist(), float(np.float32(1.0 / math.sqrt(d))), causal, dtype, f64(do))
+    within("out", out, want["out"])
+    within("lse", lse, want["lse"])
+    for name, g in zip(("dq", "dk", "dv"), B.packed_attention_bwd(q, k, v, out, do, lse, qs, ks, causal=causal)):
+        within(name, g, want[name])
+    ck, cv, table = pages(gen, kl, page, 2, d, dtype)
+    have = torch.tensor(kl, dtype=torch.int32, device="cuda")
+    B.paged_append(k, v, ck, cv, table, ks, have)
+    within("paged", B.paged_attention(q, ck, cv, table, qs, have, causal=causal), want["out"])
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+def test_large_values_do_not_overflow(B, dtype, d):
+    """Values around 2^95 and logits that grow along the row."""
+    gen = torch.Generator().manual_seed(21)
+    n = 900
+    q, k, v = (tokens(gen, n, 2, d, dtype, "token", s) for s in (1.0, 2.0, 2.0 ** 95))
+    k = (k.float() * torch.linspace(0.2, 3.0, n, device="cuda")[:, None, None]).to(TYPE[dtype])
+    s = starts([n])
+    want = S.packed(f64(q), f64(k), f64(v), [0, n], [0, n], float(np.float32(1.0 / math.sqrt(d))), True, dtype)
+    within("out", B.packed_attention(q, k, v, s), want["out"])
+    ck, cv, table = pages(gen, [n], 16, 2, d, dtype)
+    have = torch.tensor([n], dtype=torch.int32, device="cuda")
+    B.paged_append(k, v, ck, cv, table, s, have)
+    within("paged", B.paged_attention(q[-3:], ck, cv, table, starts([3]), have), (want["out"][0][-3:], want["out"][1][-3:]))
+    within("paged", B.paged_attention(q[-300:], ck, cv, table, starts([300]), have), (want["out"][0][-300:], want["out"][1][-300:]))
