@@ -215,10 +215,14 @@ PagedPlan paged_plan(long long table_keys, int n_seqs, long long tokens, int hea
   p.few = rows <= 32LL * n_seqs;
   const long long blocks = tile_bound(tokens, group, p.few ? 32 : 128, n_seqs) * heads_kv;
   // Few rows: small workgroups that stream the cache, eight for every compute unit in turn (16 tokens over up to 16,384 keys: four 145 us, eight
-  // 136, sixteen 143).  Many: two on a unit at once, and no more ranges than one such round holds (a frame over 21 frames: 600 workgroups
-  // 131 us, 480 107).
-  const long long shortest = p.few ? 256 : 512;
-  long long r = p.few ? (8LL * compute_units() + blocks - 1) / blocks : 2LL * compute_units() / blocks;
+  // 136, sixteen 143).
+  // Many, two on a unit at once: as many ranges as one such round holds if those are three or more, else up to five, for four rounds, whose pieces of
+  // different length even out (chunks of up to 390 tokens over up to 8190, 12 heads, d = 128, us by ranges: 120 workgroups a range, 4 106, 5 128, 8
+  // 120; 180, 2 171, 5 148, 8 157; 290, 1 296, 2 177, 5 179, 8 191; 600, 1 325, 4 279, 8 312; 1200, 1 503, 2 454, 4 451, 8 536).
+  const long long shortest = p.few ? 256 : 512, slots = 2LL * compute_units();
+  long long r = 4 * slots;
+  if (!p.few && slots / blocks >= 3) r = slots / blocks;
+  else r = p.few ? (r + blocks - 1) / blocks : r / blocks < 5 ? (r + blocks - 1) / blocks : 5;
   if (r > (table_keys + shortest - 1) / shortest) r = (table_keys + shortest - 1) / shortest;
   if (r < 1) r = 1;
   p.ranges = r > 64 ? 64 : (int)r;

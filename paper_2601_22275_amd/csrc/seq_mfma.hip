@@ -48,8 +48,8 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
   constexpr int BQ = 32 * W2;
   auto swz = [](int row) { return G::swz(row); };
   extern __shared__ __attribute__((aligned(16))) char smem[];  // [K|V][NSLOT][BT rows][2 D bytes]
-  __shared__ int entry[PAGED ? 4 : 1][64];
-  __shared__ RowAt row_at[PAGED ? 4 : 1][BT];
+  __shared__ int entry[PAGED ? W2 : 1][64];
+  __shared__ RowAt row_at[PAGED ? 2 * W2 : 1][BT];
 
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -101,21 +101,22 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
   const bf16_t* kbase = P.k.p + kvh * P.k.h + (PAGED ? 0LL : (long long)(k_begin + k0) * P.k.t);
   const bf16_t* vbase = P.v.p + kvh * P.v.h + (PAGED ? 0LL : (long long)(k_begin + k0) * P.v.t);
   // Packed keys: a tile's address is wave-uniform, a lane's place in it a 32-bit offset (the host keeps a tile's rows within 2^31 bytes).
-  // Pages: rows lie anywhere.  Their addresses are formed once each, by one wave for all, a tile ahead of their loads (row_at), from entries of
-  // the table that came to LDS a tile before that (entry).  (64-bit products in every lane that loads: 16,384 causal tokens 861 TFLOP/s, so 947.)
+  // Pages: rows lie anywhere.  Their addresses are formed once each: every fourth tile each wave forms those of one of the next four (row_at), from
+  // entries of the table that came to LDS four tiles before (entry).  Sixty-four-bit products in every lane that loads cost 16,384 causal
+  // tokens 861 TFLOP/s in place of 947.
   const int row_k = (int)(2 * P.k.t), row_v = (int)(2 * P.v.t);  // bytes (packed keys)
   const int last_key = max(nk - 1, 0);
   auto key_of = [&](int t) __attribute__((always_inline)) { return min(k0 + t * BT + lane % BT, last_key); };
-  auto fetch_entries = [&](int t) __attribute__((always_inline)) {  // by one wave; past the last tile: the last key's, never used
+  auto fetch_entries = [&](int t) __attribute__((always_inline)) {  // past the last tile: the last key's, never used
     const int* e = P.table + w.seq * P.table_stride + key_of(t) / P.page_size;
-    const unsigned dst = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long long)(__attribute__((address_space(3))) char*)&entry[t & 3][0]);
+    const unsigned dst = __builtin_amdgcn_readfirstlane((unsigned)(unsigned long long)(__attribute__((address_space(3))) char*)&entry[wave][0]);
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(e), "s"(dst) : "memory", "m0");
   };
-  auto prepare_rows = [&](int t) __attribute__((always_inline)) {  // by one wave
-    const int e = entry[t & 3][lane];
+  auto prepare_rows = [&](int t) __attribute__((always_inline)) {
+    const int e = entry[wave][lane];
     const long long page = e < 0 || e >= P.n_pages ? 0 : e;
     const int slot = key_of(t) % P.page_size;
-    row_at[t & 3][lane % BT] = RowAt{kbase + page * P.k.page + slot * P.k.t, vbase + page * P.v.page + slot * P.v.t};
+    row_at[t & 7][lane % BT] = RowAt{kbase + page * P.k.page + slot * P.k.t, vbase + page * P.v.page + slot * P.v.t};
   };
   auto issue_tile = [&](int t) __attribute__((always_inline)) {  // into slot t & 3
     const unsigned kb = lds_base + (t & (NSLOT - 1)) * TILE_BYTES;
@@ -128,7 +129,7 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
       const unsigned dst = __builtin_amdgcn_readfirstlane(kb + (RPI * W2 * r + RPI * wave) * ROW_BYTES);
       const unsigned vdst = dst + V_OFF;
       if (PAGED) {
-        const RowAt at = row_at[t & 3][row];
+        const RowAt at = row_at[t & 7][row];
         const bf16_t *ka = at.k + st_lc * 8, *va = at.v + st_lc * 8;
         if (st_on) {
           asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(ka), "s"(dst) : "memory", "m0");
@@ -158,7 +159,8 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
   if (PAGED && ntiles > 0) {
     fetch_entries(wave);  // tiles 0 .. 3
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    prepare_rows(wave);  // (tile 3's again in the first iteration)
+    prepare_rows(wave);
+    fetch_entries(W2 + wave);
     __syncthreads();
   }
   if (ntiles > 0) issue_tile(0);
@@ -382,9 +384,11 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();  // tile tt + 1 has landed for everyone; everyone is done with tile tt - 2
     }
-    if (PAGED && (tt & (W2 - 1)) == wave) prepare_rows(tt + 3);
+    if (PAGED && tt % W2 == 0) {
+      prepare_rows(tt + W2 + wave);
+      fetch_entries(tt + 2 * W2 + wave);
+    }
     if (tt + 2 < ntiles) issue_tile(tt + 2);
-    if (PAGED && ((tt + 1) & (W2 - 1)) == wave) fetch_entries(tt + 4);
   };
   if (ntiles > 0) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
