@@ -445,6 +445,8 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
   }
 
   // ---- tiles that some row sees in part -------------------------------------------------------------------------------------------
+  // what the wave's first and last row see of the range
+  const int wave_least = min(__builtin_amdgcn_readfirstlane(limit), nkeys), wave_most = min(__builtin_amdgcn_readfirstlane(__shfl(limit, 31)), nkeys);
   for (; t < ntiles; ++t) {
     next_tile(t);
     if (!active) continue;
@@ -452,23 +454,22 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
     for (int sub = 0; sub < BT / 32; ++sub) {
       const int off = (t & 3) * TILE_BYTES + sub * 32 * ROW_BYTES;
       const int first = t * BT + 32 * sub;
-      if (first >= nkeys) break;
+      if (first >= wave_most) break;
+      const bool part = first + 32 > wave_least;
+      const bool odd = part && odd_values<ROW_BYTES>(lds_base + V_OFF + off);
       f32x16 s;
       bf16x8 pb[2];
       plain_logits(off, s);
-      bool move = false;
-      float top;
-      const int left = min(limit, nkeys) - first - 4 * g;
+      if (part) {
+        const int left = min(limit, nkeys) - first - 4 * g;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < left ? s[r] : -INFINITY;
-      top = subtile_max(s) * sc;
-      move = move || top > msc + MOVE_ALONG2;
-      if (__any(move)) {
-        move_reference(top, 0.f);
+        for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < left ? s[r] : -INFINITY;
       }
+      const float top = subtile_max(s) * sc;
+      if (__any(top > msc + MOVE_ALONG2)) move_reference(top, 0.f);
       plain_weights(s, pb);
       add_sums();
-      if (!odd_values<ROW_BYTES>(lds_base + V_OFF + off)) {
+      if (!odd) {
         plain_products(off, pb);
         wait_products();
         continue;
