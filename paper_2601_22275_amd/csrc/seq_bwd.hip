@@ -529,12 +529,13 @@ hipError_t launch(const SeqParams<bf16_t>& P, hipStream_t st) {
 
 }  // namespace
 
-// Ranges the rows of queries are cut into for dK and dV: enough for two workgroups of 128 keys on every compute unit (which holds one), but
-// none below 512 rows of an average sequence.  Forward and backward, one range / two a unit: 4 clips of up to 3157 rows on texts of up to 512 keys, 10 heads of
-// 64: 104 / 87 us; 2048 causal tokens, 12 heads on 2, d = 64: 267 / 125; 3 x 4096, 12 heads on 4, d = 128 (344 workgroups) takes one either way.
+// Ranges the rows of queries are cut into for dK and dV: up to three workgroups of 128 keys for every compute unit (which holds one), but none below
+// 512 rows of an average sequence.  Forward and backward, us by workgroups a unit, one / two / three / four: 3 x 4096 tokens, 12 heads on 4, d =
+// 128 692 / 691 / 659 / 661, without a mask 1185 / 1186 / 1137 / 1136; one sequence of 4096 532 / 396 / 390 / 402; 2 x 2000, 12 heads on 12 197 / 197 /
+// 197 / 256; 4 clips of up to 3157 rows on texts of up to 512 keys, 10 heads of 64 107 / 87 / 90 / 90.
 int seq_bwd_ranges(int n_seqs, long long tokens_q, long long tokens_k, int heads_kv, int group) {
   const long long blocks = tile_bound(tokens_k, 1, 32 * NT, n_seqs) * heads_kv;
-  long long r = 2LL * compute_units() / (blocks > 0 ? blocks : 1);
+  long long r = 3LL * compute_units() / (blocks > 0 ? blocks : 1);
   const long long most = tokens_q * group / n_seqs / 512;
   if (r > most) r = most;
   return r < 2 ? 1 : r > 32 ? 32 : (int)r;
