@@ -6,6 +6,8 @@
 // heads of the token that its workgroup handles, four heads' loads in flight.  The angle is reduced in 64 bits, in full turns: a
 // position times a frequency in 32 bits is off by 2^-24 of the angle, 0.06 radians at a million; the multiplication, the nearest whole turn
 // and the difference are three fp64 instructions a pair, and what is left is at most half a turn, for which 32 bits are enough.
+// q and k of 32,760 tokens, 12 heads of 128 each, bf16 (403 MB): 81 us, 5.0 TB/s, the rate of a large copy; two frames of 3 streams into pages (93 MB)
+// 20 us; 24 tokens 7 us, a chain of dependent loads.
 #include "seq.h"
 
 namespace vm {

@@ -497,3 +497,22 @@ def test_large_values_do_not_overflow(B, dtype, d):
     B.paged_append(k, v, ck, cv, table, s, have)
     within("paged", B.paged_attention(q[-3:], ck, cv, table, starts([3]), have), (want["out"][0][-3:], want["out"][1][-3:]))
     within("paged", B.paged_attention(q[-300:], ck, cv, table, starts([300]), have), (want["out"][0][-300:], want["out"][1][-300:]))
+
+
+@pytest.mark.parametrize("d,kv,group,ql,kl,causal", [(64, 2, 2, [1500, 700], [200, 130], False), (128, 1, 2, [1300], None, True), (72, 1, 4, [700, 0, 900], [40, 10, 333], True)])
+def test_gradients_of_keys_that_many_rows_see(B, d, kv, group, ql, kl, causal):
+    """Few keys under many rows: the rows are cut into ranges whose sums meet in memory.  The first two tokens and the last belong to no sequence."""
+    gen = torch.Generator().manual_seed(d)
+    kl = ql if kl is None else kl
+    assert B.lib().vmonarch_packed_attention_bwd_workspace_bytes(len(ql), sum(ql), sum(kl), kv * group, kv, d) > 16 * sum(ql) * kv * group  # ranges
+    q, do = (tokens(gen, sum(ql) + 3, kv * group, d, "bf16", "head") for _ in range(2))
+    k, v = (tokens(gen, sum(kl) + 3, kv, d, "bf16", "fused") for _ in range(2))
+    qs, ks = starts(ql, 2), starts(kl, 2)
+    out, lse = B.packed_attention(q, k, v, qs, ks, causal=causal, lse=True)
+    dk, dv = torch.full_like(k, 3.0), torch.full_like(v, 3.0)
+    dq, dk, dv = B.packed_attention_bwd(q, k, v, out, do, lse, qs, ks, causal=causal, dk=dk, dv=dv)
+    want = S.packed(f64(q), f64(k), f64(v), qs.tolist(), ks.tolist(), float(np.float32(1.0 / math.sqrt(d))), causal, "bf16", f64(do))
+    for name, g in (("dq", dq), ("dk", dk), ("dv", dv)):
+        within(name, g[2:-1], tuple(x[2:-1] for x in want[name]))
+    for x in (dk, dv):
+        assert (x[:2] == 3).all() and (x[-1] == 3).all()
