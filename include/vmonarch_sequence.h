@@ -10,7 +10,8 @@
  *     the call only.
  *   - Calls without suffix take bfloat16 token tensors, `_f32` twins float32; statistics are float32.
  *   - The current device is the one that holds the tensors.
- *   - 1 <= d <= 256, heads_q a multiple of heads_kv; query head h reads key head h / (heads_q / heads_kv).
+ *   - 1 <= d <= 256, heads_q a multiple of heads_kv; query head h reads key head h / (heads_q / heads_kv).  Tokens, tokens times
+ *     heads_q / heads_kv, and the tokens a row of a table has room for are at most 2^31 - 65536 each, sequences at most 2^30 - 1.
  *   - Sequences: sequence s of n_seqs holds the packed tokens starts[s] .. starts[s + 1] - 1 (int32, DEVICE memory,
  *     n_seqs + 1 entries, non-decreasing).  A sequence may be empty.  The host cannot see these: entries are clamped to
  *     [0, tokens] on the device, and rows of a tensor that belong to no sequence are neither read nor written.

@@ -16,6 +16,9 @@ int hip_result(hipError_t e, const char* what) {
   return e == hipSuccess ? VMONARCH_OK : api_fail(VMONARCH_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
+// Kernels count tokens, packed rows and keys in 32 bits, and look some tiles (and 64 ranges, each rounded up to 64 keys) past the last
+constexpr long long kMostTokens = 0x7fff0000LL;
+
 struct Checked {
   bool aligned = true;  // every row of every tensor seen starts on a 16-byte boundary
 };
@@ -39,8 +42,9 @@ int check_sizes(int n_seqs, long long tokens_q, long long tokens_k, int heads_q,
   if (heads_q % heads_kv != 0) return api_fail(VMONARCH_ERR_INVALID_ARG, "heads_q=%d is no multiple of heads_kv=%d", heads_q, heads_kv);
   if (d > 256) return api_fail(VMONARCH_ERR_UNSUPPORTED, "d=%d exceeds 256", d);
   if (heads_q > 65535) return api_fail(VMONARCH_ERR_UNSUPPORTED, "heads_q=%d exceeds 65535", heads_q);
-  if (tokens_q > 0x7fffff00LL || tokens_k > 0x7fffff00LL) return api_fail(VMONARCH_ERR_UNSUPPORTED, "more than 2^31 - 256 tokens");
-  if (tokens_q * (heads_q / heads_kv) > 0x7fffff00LL) return api_fail(VMONARCH_ERR_UNSUPPORTED, "more rows of queries than one launch takes");
+  if (n_seqs > 0x3fffffff) return api_fail(VMONARCH_ERR_UNSUPPORTED, "more than 2^30 - 1 sequences");
+  if (tokens_q > kMostTokens || tokens_k > kMostTokens) return api_fail(VMONARCH_ERR_UNSUPPORTED, "more than 2^31 - 65536 tokens");
+  if (tokens_q * (heads_q / heads_kv) > kMostTokens) return api_fail(VMONARCH_ERR_UNSUPPORTED, "more rows of queries than one launch takes");
   return VMONARCH_OK;
 }
 
@@ -61,8 +65,8 @@ int check_cache(const vmonarch_cache* c, int heads_kv, size_t elem, bool output,
   if (c->n_pages < 1 || c->page_size < 1 || c->table_width < 1)
     return api_fail(VMONARCH_ERR_INVALID_ARG, "sizes must be positive (n_pages=%d page_size=%d table_width=%d)", c->n_pages, c->page_size, c->table_width);
   if (c->table_stride < 0) return api_fail(VMONARCH_ERR_INVALID_ARG, "negative cache.table_stride");
-  if ((long long)c->table_width * c->page_size > 0x7fffff00LL)
-    return api_fail(VMONARCH_ERR_UNSUPPORTED, "a row of the table has room for more than 2^31 - 256 tokens");
+  if ((long long)c->table_width * c->page_size > kMostTokens)
+    return api_fail(VMONARCH_ERR_UNSUPPORTED, "a row of the table has room for more than 2^31 - 65536 tokens");
   int rc = check_starts(c->table, "cache.table");
   if (!rc) rc = check_starts(c->lengths, "cache.lengths");
   if (rc) return rc;
@@ -134,7 +138,7 @@ int rotary_impl(const vmonarch_tokens* q, const vmonarch_tokens* q_out, int head
     return api_fail(VMONARCH_ERR_INVALID_ARG, "sizes out of range (tokens=%lld heads=%d, %d d=%d)", tokens, heads_q, heads_k, d);
   if (d > 256) return api_fail(VMONARCH_ERR_UNSUPPORTED, "d=%d exceeds 256", d);
   if (heads_q > 65535 || heads_k > 65535) return api_fail(VMONARCH_ERR_UNSUPPORTED, "more than 65535 heads");
-  if (tokens > 0x7fffff00LL) return api_fail(VMONARCH_ERR_UNSUPPORTED, "more than 2^31 - 256 tokens");
+  if (tokens > kMostTokens) return api_fail(VMONARCH_ERR_UNSUPPORTED, "more than 2^31 - 65536 tokens");
   if ((k == nullptr) != (heads_k == 0) || (k == nullptr) != (k_out == nullptr))
     return api_fail(VMONARCH_ERR_INVALID_ARG, "k, k_out and heads_k must be given together or not at all");
   int pairs = 0;

@@ -152,3 +152,16 @@ def test_binding_refuses_what_is_not_a_device_tensor():
         binding.packed_attention(x, x, x, s)
     with pytest.raises(binding.VMonarchError):
         binding.rotary(x, None, s, binding.rotary_plan([2]))
+
+
+def test_counts_at_the_edge_of_32_bits():
+    # kernels look some tiles past the last token, so the last 2^16 counts are refused too
+    refuses(UNSUPPORTED, attend(tk=2 ** 31 - 65535), "tokens")
+    refuses(UNSUPPORTED, attend(tq=2 ** 30 - 32767, hq=4, hk=2), "one launch")
+    refuses(UNSUPPORTED, attend(n=2 ** 30), "sequences")
+    lib = binding.lib()
+    wide = cache(table_width=2 ** 20 - 31, page_size=2 ** 11)  # 2^31 - 63488
+    refuses(UNSUPPORTED, lib.vmonarch_paged_attention(T(), wide, T(1 << 19), INT, 1, 8, 4, 2, 64, 1.0, 1, None, 0, None), "room")
+    refuses(UNSUPPORTED, lib.vmonarch_paged_append(T(), T(1 << 18), wide, INT, 1, 8, 2, 64, None, None, 8, None), "room")
+    plan = binding.rotary_plan([16])
+    refuses(UNSUPPORTED, lib.vmonarch_rotary(T(), T(1 << 18), 1, None, None, 0, 2 ** 31 - 65535, 64, INT, 8, ctypes.byref(plan), 0, None), "tokens")
