@@ -68,8 +68,9 @@ struct Span {
 __device__ __forceinline__ int start_of(const int* starts, int s, int tokens) { return min(max(starts[s], 0), tokens); }
 
 // Tiles of BM rows (tokens * rows_per_token) of all sequences in one row of workgroups.  Sequence s owns tiles f(s) .. f(s+1) - 1 with
-// f(s) = floor(starts[s] rows_per_token / BM) + s: at least the ceil(rows / BM) it needs, so the host can launch f(n) =
-// floor(tokens rows_per_token / BM) + n of them without seeing the lengths.  The sequence of tile `t` is found by all lanes of a wave at once.
+// f(s) = floor(starts[s] rows_per_token / BM) + s: at least the ceil(rows / BM) it needs, and the last one needs none from
+// ceil(tokens rows_per_token / BM) + n - 1 on: the host launches that many without seeing the lengths.  The sequence of tile `t` is found by all
+// lanes of a wave at once.
 __device__ __forceinline__ Span find_tile(const int* starts, int n_seqs, int tokens, int rows_per_token, int BM, int t) {
   const int lane = threadIdx.x & 63;
   int s = 0;
@@ -134,8 +135,8 @@ __device__ __forceinline__ Span find_tile_by_work(const int* starts, int n_seqs,
   return w;
 }
 
-// Upper bound of the tiles of all sequences (see find_tile)
-inline long long tile_bound(long long tokens, int rows_per_token, int BM, int n_seqs) { return tokens * rows_per_token / BM + n_seqs; }
+// Upper bound of the tiles of all sequences (see find_tile); one sequence: what it needs
+inline long long tile_bound(long long tokens, int rows_per_token, int BM, int n_seqs) { return (tokens * rows_per_token + BM - 1) / BM + n_seqs - 1; }
 
 // Keys of sequence s: where they begin (packed) and how many there are
 template <typename E>

@@ -222,11 +222,22 @@ PagedPlan paged_plan(long long table_keys, int n_seqs, long long tokens, int hea
   // 136, sixteen 143).
   // Many, two on a unit at once: as many ranges as one such round holds if those are three or more, else up to five, for four rounds, whose pieces of
   // different length even out (chunks of up to 390 tokens over up to 8190, 12 heads, d = 128, us by ranges: 120 workgroups a range, 4 106, 5 128, 8
-  // 120; 180, 2 171, 5 148, 8 157; 290, 1 296, 2 177, 5 179, 8 191; 600, 1 325, 4 279, 8 312; 1200, 1 503, 2 454, 4 451, 8 536).
+  // 120; 180, 2 171, 5 148, 8 157; 290, 1 296, 2 177, 5 179, 8 191; 600, 1 325, 4 279, 8 312; 1200, 1 503, 2 454, 4 451, 8 536).  The pieces of one
+  // sequence are alike: as many ranges, up to five, as make rounds / ranges least, with what the partial results cost (over 8,190 to 32,768
+  // keys, us: 276 workgroups a range, 2 665, 3 501, 4 532, 5 473; 504, 1 366, 2 414, 5 445; 769, 1 1752, 2 1630, 3 1666, 5 1721).
   const long long shortest = p.few ? 256 : 512, slots = 2LL * compute_units();
   long long r = 4 * slots;
   if (!p.few && slots / blocks >= 3) r = slots / blocks;
-  else r = p.few ? (r + blocks - 1) / blocks : r / blocks < 5 ? (r + blocks - 1) / blocks : 5;
+  else if (!p.few && n_seqs == 1) {
+    double least = 0;
+    for (int x = 1; x <= 5; ++x) {
+      const double rounds = (double)((blocks * x + slots - 1) / slots) / x, partial = x == 1 ? 0 : (0.1 + 0.03 * x) * blocks / slots;
+      if (x == 1 || rounds + partial < least) {
+        least = rounds + partial;
+        r = x;
+      }
+    }
+  } else r = p.few ? (r + blocks - 1) / blocks : r / blocks < 5 ? (r + blocks - 1) / blocks : 5;
   if (r > (table_keys + shortest - 1) / shortest) r = (table_keys + shortest - 1) / shortest;
   if (r < 1) r = 1;
   p.ranges = r > 64 ? 64 : (int)r;
