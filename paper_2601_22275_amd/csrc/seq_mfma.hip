@@ -216,13 +216,25 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
   };
 
   // ---- the MFMAs, as inline assembly: logits in ordinary registers, products in accumulation registers --------------------------------
+  // A vector instruction's result takes two issue slots to reach an MFMA; the plain forms wait for them themselves (the compiler may place copies
+  // right in front), the pipeline's operands are older.
   auto mfma_first = [&](f32x16& acc, const bf16x8& a, const bf16x8& b) __attribute__((always_inline)) {
-    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(acc) : "v"(a), "v"(b));
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(acc) : "v"(a), "v"(b));
   };
   auto mfma_v = [&](f32x16& acc, const bf16x8& a, const bf16x8& b) __attribute__((always_inline)) {
-    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(a), "v"(b));
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(a), "v"(b));
   };
   auto mfma_a = [&](f32x16& acc, const bf16x8& a, const bf16x8& b) __attribute__((always_inline)) {
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+  };
+
+  auto pipe_first = [&](f32x16& acc, const bf16x8& a, const bf16x8& b) __attribute__((always_inline)) {
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(acc) : "v"(a), "v"(b));
+  };
+  auto pipe_v = [&](f32x16& acc, const bf16x8& a, const bf16x8& b) __attribute__((always_inline)) {
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(a), "v"(b));
+  };
+  auto pipe_a = [&](f32x16& acc, const bf16x8& a, const bf16x8& b) __attribute__((always_inline)) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
   };
 
@@ -253,9 +265,9 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
   };
   auto issue = [&](auto gc, f32x16 &snext, bf16x8 (&pbprev)[2]) __attribute__((always_inline)) {
     constexpr int GI = decltype(gc)::value;
-    if constexpr (GI == 0) mfma_first(snext, ring[GI % RING], qreg[GI]);
-    else if constexpr (GI < KS) mfma_v(snext, ring[GI % RING], qreg[GI]);
-    else mfma_a(oacc[(GI - KS) % CT], ring[GI % RING], pbprev[(GI - KS) / CT]);
+    if constexpr (GI == 0) pipe_first(snext, ring[GI % RING], qreg[GI]);
+    else if constexpr (GI < KS) pipe_v(snext, ring[GI % RING], qreg[GI]);
+    else pipe_a(oacc[(GI - KS) % CT], ring[GI % RING], pbprev[(GI - KS) / CT]);
   };
 
   typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
@@ -493,7 +505,6 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
             __builtin_memcpy(&a, a32, 16);
             const bool v = first + 16 * c + i < min(limit, nkeys);
             f32x16 one;
-            asm volatile("s_nop 4");
             mfma_first(one, a, pb[c]);
             SQ_MFMA_RESULT_WAIT();
             SQ_FENCE();
