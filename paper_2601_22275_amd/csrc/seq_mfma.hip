@@ -404,6 +404,9 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
     }
     if (tt + 2 < ntiles) issue_tile(tt + 2);
   };
+  // the queries are here: left to itself the compiler waits for them in the loop, and with them for the tile just requested
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qreg[ks]));
   if (ntiles > 0) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
