@@ -126,6 +126,9 @@ __global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) seq_token_kernel(Seq
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qreg[ks] = 16 * ks + 8 * g < P.d ? *reinterpret_cast<const bf16x8*>(qp + 16 * ks) : zero;
     limit = min(P.causal ? (int)min(max(more + 1 + tok, 0LL), (long long)nk) : nk, see_most);
+    // the queries are here: left to itself the compiler waits for them in the loop, and with them for the sub-tiles under way
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qreg[ks]));
   }
 
   typedef __attribute__((address_space(3))) const bf16x8* lds_b128_ptr;
