@@ -154,8 +154,9 @@ __global__ void __launch_bounds__(256 * parts<D>(), D == 256 ? 1 : 2) seq_genera
     }
   }
   const float sc = P.scale * LOG2E;
-  // what an owner row needs: queries: the number of keys they see (and their statistics); keys: the first token that sees them
+  // what an owner row needs: queries: the number of keys they see (and their statistics); keys: the first packed row that sees them
   int limit = 0;
+  const long long first_row = MODE == GRAD_KV && P.causal ? max((orow - more) * group, 0LL) : 0;
   float o_lse = 0.f, o_delta = 0.f;
   if (MODE != GRAD_KV) {
     limit = !ovalid ? 0 : P.causal ? min(max(more + 1 + (int)(orow / group), 0), nk) : nk;
@@ -231,6 +232,12 @@ __global__ void __launch_bounds__(256 * parts<D>(), D == 256 ? 1 : 2) seq_genera
   float d_sum = 0.f;
   // (past the last tile the half that has none left multiplies zeros)
   if (ntiles > 0) fetch(part);
+  // the owner rows are here: left to itself the compiler waits for them in the loop, and with them for the tile just requested
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    asm volatile("" : "+v"(r1[j]));
+    if (BWD) asm volatile("" : "+v"(r2[BWD ? j : 0]));
+  }
   for (int tile = part; tile - part < ntiles; tile += PARTS) {
     const long long base = s0 + (long long)tile * BN;
     bool odd_value = false;
@@ -279,6 +286,14 @@ __global__ void __launch_bounds__(256 * parts<D>(), D == 256 ? 1 : 2) seq_genera
         }
       }
     }
+    // the tile's rows from .. to - 1 go with the owner row
+    int from = 0, to;
+    if (MODE == GRAD_KV) {
+      from = (int)min(max(first_row - base, 0LL), (long long)BN);
+      to = ovalid ? (int)min(s1 - base, (long long)BN) : 0;
+    } else {
+      to = (int)min(max(min((long long)limit, s1) - base, 0LL), (long long)BN);
+    }
     float p[2][4], ds[2][4], keep = 1.f;
     unsigned sees = 0;  // bit 4 kb + r
     if (MODE == FORWARD) {
@@ -287,7 +302,7 @@ __global__ void __launch_bounds__(256 * parts<D>(), D == 256 ? 1 : 2) seq_genera
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const bool v = base + 16 * kb + 4 * g + r < min((long long)limit, s1);
+          const bool v = 16 * kb + 4 * g + r < to;
           sees |= (unsigned)v << (4 * kb + r);
           s[kb][r] = v ? s[kb][r] * sc : -INFINITY;
           top = fmaxf(top, s[kb][r]);
@@ -313,15 +328,12 @@ __global__ void __launch_bounds__(256 * parts<D>(), D == 256 ? 1 : 2) seq_genera
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int sr = 16 * kb + 4 * g + r;
-          bool v;
+          const bool v = sr >= from && sr < to;
           float lse2, delta;
           if (MODE == GRAD_Q) {
-            v = base + sr < limit;
             lse2 = o_lse;
             delta = o_delta;
           } else {
-            const long long row = base + sr;
-            v = ovalid && row < s1 && (!P.causal || orow <= (long long)more + row / group);
             lse2 = st_lse[MODE == GRAD_KV ? sr : 0];
             delta = st_delta[MODE == GRAD_KV ? sr : 0];
           }
@@ -344,23 +356,20 @@ __global__ void __launch_bounds__(256 * parts<D>(), D == 256 ? 1 : 2) seq_genera
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int ct = 0; ct < 4; ++ct) sum[x][c][ct] = MODE == FORWARD ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[x][c][ct];
+    auto products = [&](auto slow_c) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * kb + 4 * g + r;
+        for (int r = 0; r < 4; ++r) {
+          const int row = 16 * kb + 4 * g + r;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const f32x4 a2 = *reinterpret_cast<const f32x4*>(&x2[row][64 * c + 4 * li]);
-          if (MODE == FORWARD) {
-            if (!slow) {
-#pragma unroll
-              for (int ct = 0; ct < 4; ++ct) sum[0][c][ct] = mfma(a2[ct], p[kb][r], sum[0][c][ct]);
-            } else {
+          for (int c = 0; c < NC; ++c) {
+            const f32x4 a2 = *reinterpret_cast<const f32x4*>(&x2[row][64 * c + 4 * li]);
+            if (decltype(slow_c)::value) {
               // one key at a time, added only to the rows that see it: zero times infinity stays out of the others
 #pragma unroll
               for (int gg = 0; gg < 4; ++gg) {
-                const bool v = base + 16 * kb + 4 * gg + r < min((long long)limit, s1);
+                const bool v = 16 * kb + 4 * gg + r < to;
 #pragma unroll
                 for (int ct = 0; ct < 4; ++ct) {
                   const f32x4 one = mfma(g == gg ? a2[ct] : 0.f, p[kb][r], f32x4{0.f, 0.f, 0.f, 0.f});
@@ -368,21 +377,26 @@ __global__ void __launch_bounds__(256 * parts<D>(), D == 256 ? 1 : 2) seq_genera
                   for (int e = 0; e < 4; ++e) sum[0][c][ct][e] += v ? one[e] : 0.f;
                 }
               }
-            }
-          } else if (MODE == GRAD_Q) {
-            const f32x4 a1 = *reinterpret_cast<const f32x4*>(&x1[row][64 * c + 4 * li]);
+            } else if (MODE == FORWARD) {
 #pragma unroll
-            for (int ct = 0; ct < 4; ++ct) sum[0][c][ct] = mfma(a1[ct], ds[kb][r], sum[0][c][ct]);
-          } else {
-            const f32x4 a1 = *reinterpret_cast<const f32x4*>(&x1[row][64 * c + 4 * li]);
+              for (int ct = 0; ct < 4; ++ct) sum[0][c][ct] = mfma(a2[ct], p[kb][r], sum[0][c][ct]);
+            } else if (MODE == GRAD_Q) {
+              const f32x4 a1 = *reinterpret_cast<const f32x4*>(&x1[row][64 * c + 4 * li]);
 #pragma unroll
-            for (int ct = 0; ct < 4; ++ct) {
-              sum[0][c][ct] = mfma(a1[ct], ds[kb][r], sum[0][c][ct]);
-              sum[NACC - 1][c][ct] = mfma(a2[ct], p[kb][r], sum[NACC - 1][c][ct]);
+              for (int ct = 0; ct < 4; ++ct) sum[0][c][ct] = mfma(a1[ct], ds[kb][r], sum[0][c][ct]);
+            } else {
+              const f32x4 a1 = *reinterpret_cast<const f32x4*>(&x1[row][64 * c + 4 * li]);
+#pragma unroll
+              for (int ct = 0; ct < 4; ++ct) {
+                sum[0][c][ct] = mfma(a1[ct], ds[kb][r], sum[0][c][ct]);
+                sum[NACC - 1][c][ct] = mfma(a2[ct], p[kb][r], sum[NACC - 1][c][ct]);
+              }
             }
           }
         }
-      }
+    };
+    if (slow) products(std::bool_constant<MODE == FORWARD>{});
+    else products(std::false_type{});
 #pragma unroll
     for (int x = 0; x < NACC; ++x)
 #pragma unroll
@@ -475,10 +489,25 @@ hipError_t launch(const SeqParams<E>& P, hipStream_t st) {
   const long long tiles = MODE == GRAD_KV ? tile_bound(P.tokens_k, 1, BM, P.n_seqs) : tile_bound(P.tokens_q, P.group, BM, P.n_seqs);
   if (tiles > 0x7fffffffLL) return hipErrorInvalidValue;
   const dim3 grid((unsigned)tiles, (unsigned)P.heads_kv, (unsigned)(MODE == FORWARD && P.ranges > 1 ? P.ranges : 1));
-  if (P.d <= 64) hipLaunchKernelGGL((seq_general_kernel<E, 64, MODE>), grid, dim3(512), 0, st, P);
-  else if (P.d <= 128) hipLaunchKernelGGL((seq_general_kernel<E, 128, MODE>), grid, dim3(512), 0, st, P);
-  else hipLaunchKernelGGL((seq_general_kernel<E, 256, MODE>), grid, dim3(256), 0, st, P);
-  return hipGetLastError();
+  auto go = [&](auto dc) -> hipError_t {
+    constexpr int D = decltype(dc)::value;
+    auto kern = seq_general_kernel<E, D, MODE>;
+    // Under a causal mask a launch of up to two workgroups a unit is spread one to a unit (by more LDS than it needs): longest first, two of the
+    // longest would share one (us, one / two: 4 prompts of up to 1001 64 / 87, one of 3000 168 / 248; 8 of up to 1001, 900 workgroups 96 / 79;
+    // without a mask 113 / 94).
+    int pad = 0;
+    if (D == 64 && P.causal && (long long)grid.x * grid.y * grid.z <= 2LL * compute_units()) {
+      pad = 48 * 1024;
+      static std::atomic<unsigned long long> done{0};
+      const hipError_t e = allow_lds((const void*)kern, pad, &done);
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kern, grid, dim3(256 * parts<D>()), pad, st, P);
+    return hipGetLastError();
+  };
+  if (P.d <= 64) return go(std::integral_constant<int, 64>{});
+  if (P.d <= 128) return go(std::integral_constant<int, 128>{});
+  return go(std::integral_constant<int, 256>{});
 }
 
 }  // namespace
