@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import struct
 from ctypes import byref, c_char_p, c_float, c_int, c_size_t, c_void_p
 
 import torch
@@ -419,26 +420,34 @@ def permute_tokens(x, T, Hs, Ws, to_position_major=True, out=None):
 
 
 def _sizes(name, x):
+    """Tokens and heads of the tensor that sets the others' head size, type and device number, and those three."""
     shape = x.shape
     if len(shape) != 3:
         raise VMonarchError(f"{name}: expected [tokens, heads, d], got {tuple(shape)}")
     if not x.is_cuda:
         raise VMonarchError(f"{name}: a CUDA tensor is needed")
-    return shape
+    n, heads, d = shape
+    return n, heads, (d, x.dtype, x.get_device())
+
+
+# Tokens and Cache as bytes, which ctypes passes by address: half the time of a structure and its reference
+_pack_tokens = struct.Struct("@Pqq").pack
+_pack_cache = struct.Struct("@PP6qiiPqiP").pack
 
 
 def _tokens(name, x, like):
-    """The descriptor of token tensor x, checked against the type, device and head size of `like`."""
-    shape, stride = x.shape, x.stride()
-    if len(shape) != 3 or x.dtype is not like.dtype or x.get_device() != like.get_device() or shape[2] != like.shape[2]:
+    """The descriptor of token tensor x, checked against like = (head size, type, device number)."""
+    stride = x.stride()
+    d, dtype, dev = like
+    if len(stride) != 3 or x.dtype is not dtype or x.get_device() != dev or x.shape[2] != d:
         raise VMonarchError(f"{name}: expected [tokens, heads, d] of the other tensors' type, device and head size")
-    if stride[2] != 1 and shape[2] > 1:
+    if stride[2] != 1 and d > 1:
         raise VMonarchError(f"{name}: adjacent channels are needed")
-    return byref(Tokens(x.data_ptr(), stride[0], stride[1]))
+    return _pack_tokens(x.data_ptr(), stride[0], stride[1])
 
 
-def _int32(name, x, like, shape):
-    if x.dtype is not torch.int32 or x.get_device() != like.get_device() or x.shape != shape or not x.is_contiguous():
+def _int32(name, x, dev, shape):
+    if x.dtype is not torch.int32 or x.get_device() != dev or x.shape != shape or not x.is_contiguous():
         raise VMonarchError(f"{name}: a contiguous int32 tensor of shape {tuple(shape)} on the other tensors' device is needed")
     return x.data_ptr()
 
@@ -451,12 +460,12 @@ def _same_shape(name, x, y):
 _entries = {}  # (name, type) -> function of the library
 
 
-def _run(name, like, *args):
-    """Calls an entry point on the current stream of `like`'s device."""
-    fn = _entries.get((name, like.dtype))
+def _run(name, x, like, *args):
+    """Calls an entry point for x's type on the current stream of its device; like = (head size, type, device number) of x."""
+    _, dtype, dev = like
+    fn = _entries.get((name, dtype))
     if fn is None:
-        fn = _entries[name, like.dtype] = getattr(lib(), name + _suffix(like))
-    dev = like.get_device()
+        fn = _entries[name, dtype] = getattr(lib(), name + _suffix(x))
     if dev == torch.cuda.current_device():
         rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))  # a tenth of a microsecond; the stream object takes one
     else:
@@ -481,7 +490,7 @@ def rotary_plan(axis_pairs, base=10000.0, interleaved=False, factor=1.0, context
 def rotary(q, k, positions, plan: RotaryPlan, backward=False, q_out=None, k_out=None):
     """Turns q and k ([tokens, heads, d]; k may be None) at positions (int32 [axes, tokens], or [tokens] for one axis); backward: gradients of the
     turned tensors to those of q and k.  q_out / k_out may be q / k themselves.  Returns (q_out, k_out)."""
-    n, heads, d = _sizes("q", q)
+    n, heads, like = _sizes("q", q)
     if q_out is None:
         q_out = torch.empty_like(q)
     else:
@@ -492,15 +501,15 @@ def rotary(q, k, positions, plan: RotaryPlan, backward=False, q_out=None, k_out=
             k_out = torch.empty_like(k)
         else:
             _same_shape("k_out", k_out, k)
-        dk, dko, heads_k = _tokens("k", k, q), _tokens("k_out", k_out, q), k.shape[1]
+        dk, dko, heads_k = _tokens("k", k, like), _tokens("k_out", k_out, like), k.shape[1]
         if k.shape[0] != n:
             raise VMonarchError("k: as many tokens as q are needed")
     elif k_out is not None:
         raise VMonarchError("k_out without k")
     if positions.dim() == 1:
         positions = positions[None]
-    _run("vmonarch_rotary", q, _tokens("q", q, q), _tokens("q_out", q_out, q), heads, dk, dko, heads_k, n, d,
-         _int32("positions", positions, q, (plan.axes, n)), n, byref(plan), 1 if backward else 0)
+    _run("vmonarch_rotary", q, like, _tokens("q", q, like), _tokens("q_out", q_out, like), heads, dk, dko, heads_k, n, like[0],
+         _int32("positions", positions, like[2], (plan.axes, n)), n, byref(plan), 1 if backward else 0)
     return q_out, k_out
 
 
@@ -508,8 +517,9 @@ def packed_attention(q, k, v, q_starts, k_starts=None, causal=True, scale=None, 
     """Attention over packed sequences: q [tokens_q, heads_q, d]; k, v [tokens_k, heads_kv, d]; q_starts / k_starts int32 [n_seqs + 1] (k_starts None:
     q_starts).  scale defaults to 1 / sqrt(d).  Returns out, or (out, lse) with lse float32 [heads_q, tokens_q] for packed_attention_bwd.
     Rows of no sequence are not written: bring a cleared `out` where a padded batch's tail is read later."""
-    nq, heads, d = _sizes("q", q)
+    nq, heads, like = _sizes("q", q)
     nk, kv, _ = _sizes("k", k)
+    d, _, dev = like
     if out is None:
         out = q.new_empty((nq, heads, d))
     else:
@@ -517,31 +527,33 @@ def packed_attention(q, k, v, q_starts, k_starts=None, causal=True, scale=None, 
     _same_shape("v", v, k)
     stat = torch.empty((heads, nq), dtype=torch.float32, device=q.device) if lse else None
     n = q_starts.numel()
-    qs = _int32("q_starts", q_starts, q, (n,))
-    ks = qs if k_starts is None or k_starts is q_starts else _int32("k_starts", k_starts, q, (n,))
-    _run("vmonarch_packed_attention", q, _tokens("q", q, q), _tokens("k", k, q), _tokens("v", v, q), _tokens("out", out, q),
+    qs = _int32("q_starts", q_starts, dev, (n,))
+    ks = qs if k_starts is None or k_starts is q_starts else _int32("k_starts", k_starts, dev, (n,))
+    _run("vmonarch_packed_attention", q, like, _tokens("q", q, like), _tokens("k", k, like), _tokens("v", v, like), _tokens("out", out, like),
          stat.data_ptr() if lse else None, qs, ks, n - 1, nq, nk, heads, kv, d, 1.0 / math.sqrt(d) if scale is None else scale, 1 if causal else 0)
     return (out, stat) if lse else out
 
 
 def packed_attention_bwd(q, k, v, out, d_out, lse, q_starts, k_starts=None, causal=True, scale=None, dq=None, dk=None, dv=None, workspace=None):
     """Gradients (dq, dk, dv) of packed_attention from its out and lse.  Rows of no sequence are not written (see there)."""
-    nq, heads, d = _sizes("q", q)
+    nq, heads, like = _sizes("q", q)
     nk, kv, _ = _sizes("k", k)
+    d, _, dev = like
     dq = q.new_empty((nq, heads, d)) if dq is None else dq
     dk = q.new_empty((nk, kv, d)) if dk is None else dk
     dv = q.new_empty((nk, kv, d)) if dv is None else dv
-    for name, x, y in (("v", v, k), ("out", out, q), ("d_out", d_out, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
-        _same_shape(name, x, y)
-    if lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous() or tuple(lse.shape) != (heads, nq):
+    if not (q.shape == out.shape == d_out.shape == dq.shape and k.shape == v.shape == dk.shape == dv.shape):
+        for name, x, y in (("v", v, k), ("out", out, q), ("d_out", d_out, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
+            _same_shape(name, x, y)
+    if lse.dtype is not torch.float32 or lse.get_device() != dev or not lse.is_contiguous() or lse.shape != (heads, nq):
         raise VMonarchError("lse: the log-sum-exp of packed_attention is needed, float32 [heads_q, tokens_q]")
     n = q_starts.numel()
-    qs = _int32("q_starts", q_starts, q, (n,))
-    ks = qs if k_starts is None or k_starts is q_starts else _int32("k_starts", k_starts, q, (n,))
+    qs = _int32("q_starts", q_starts, dev, (n,))
+    ks = qs if k_starts is None or k_starts is q_starts else _int32("k_starts", k_starts, dev, (n,))
     at, size = _workspace(workspace, q, "vmonarch_packed_attention_bwd_workspace_bytes", n - 1, nq, nk, heads, kv, d)
-    _run("vmonarch_packed_attention_bwd", q, _tokens("q", q, q), _tokens("k", k, q), _tokens("v", v, q), _tokens("out", out, q),
-         _tokens("d_out", d_out, q), lse.data_ptr(), _tokens("dq", dq, q), _tokens("dk", dk, q), _tokens("dv", dv, q), qs, ks, n - 1, nq, nk, heads, kv, d,
-         1.0 / math.sqrt(d) if scale is None else scale, 1 if causal else 0, None if at is None else at.data_ptr(), size)
+    _run("vmonarch_packed_attention_bwd", q, like, _tokens("q", q, like), _tokens("k", k, like), _tokens("v", v, like), _tokens("out", out, like),
+         _tokens("d_out", d_out, like), lse.data_ptr(), _tokens("dq", dq, like), _tokens("dk", dk, like), _tokens("dv", dv, like), qs, ks, n - 1, nq, nk,
+         heads, kv, d, 1.0 / math.sqrt(d) if scale is None else scale, 1 if causal else 0, None if at is None else at.data_ptr(), size)
     return dq, dk, dv
 
 
@@ -557,26 +569,26 @@ def _workspace(given, like, name, *sizes):
 
 def _cache(cache_k, cache_v, table, lengths, like, n_seqs):
     """The descriptor of a cache: cache_k, cache_v [pages, page_size, heads_kv, d] with adjacent channels, table int32 [n_seqs, width]."""
+    d, dtype, dev = like
     shape, ks, vs = cache_k.shape, cache_k.stride(), cache_v.stride()
-    if cache_v.shape != shape or len(shape) != 4 or shape[3] != like.shape[2] or ((ks[3] != 1 or vs[3] != 1) and shape[3] > 1):
+    if cache_v.shape != shape or len(shape) != 4 or shape[3] != d or ((ks[3] != 1 or vs[3] != 1) and d > 1):
         raise VMonarchError("cache_k, cache_v: expected [pages, page_size, heads, d] with adjacent channels, of the other tensors' head size")
-    dev = like.get_device()
-    if cache_k.dtype is not like.dtype or cache_v.dtype is not like.dtype or cache_k.get_device() != dev or cache_v.get_device() != dev:
+    if cache_k.dtype is not dtype or cache_v.dtype is not dtype or cache_k.get_device() != dev or cache_v.get_device() != dev:
         raise VMonarchError("cache_k, cache_v: the other tensors' type and device are needed")
     width, ts = table.shape, table.stride()
     if table.dtype is not torch.int32 or table.get_device() != dev or len(width) != 2 or width[0] != n_seqs or (ts[1] != 1 and width[1] > 1):
         raise VMonarchError("table: expected int32 [n_seqs, pages of the longest] on the other tensors' device")
-    return byref(Cache(cache_k.data_ptr(), cache_v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], shape[0], shape[1], table.data_ptr(), ts[0], width[1],
-                       _int32("lengths", lengths, like, (n_seqs,))))
+    return _pack_cache(cache_k.data_ptr(), cache_v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], shape[0], shape[1], table.data_ptr(), ts[0], width[1],
+                       _int32("lengths", lengths, dev, (n_seqs,)))
 
 
 def paged_append(k, v, cache_k, cache_v, table, q_starts, lengths, plan: RotaryPlan = None, positions=None):
     """Writes each sequence's chunk of new tokens (k, v [tokens, heads_kv, d], cut by q_starts) into the last slots of its lengths[s] tokens in the
     pages; with a plan keys are turned on the way, at `positions` or at the tokens' positions in their sequence."""
-    nk, kv, d = _sizes("k", k)
+    nk, kv, like = _sizes("k", k)
     _same_shape("v", v, k)
     n = q_starts.numel()
-    cache = _cache(cache_k, cache_v, table, lengths, k, n - 1)
+    cache = _cache(cache_k, cache_v, table, lengths, like, n - 1)
     if cache_k.shape[2] != kv:
         raise VMonarchError("cache_k: as many heads as k are needed")
     at = None
@@ -584,23 +596,25 @@ def paged_append(k, v, cache_k, cache_v, table, q_starts, lengths, plan: RotaryP
         if plan is None:
             raise VMonarchError("positions without a plan")
         positions = positions[None] if positions.dim() == 1 else positions
-        at = _int32("positions", positions, k, (plan.axes, nk))
-    _run("vmonarch_paged_append", k, _tokens("k", k, k), _tokens("v", v, k), cache, _int32("q_starts", q_starts, k, (n,)), n - 1, nk, kv, d,
+        at = _int32("positions", positions, like[2], (plan.axes, nk))
+    _run("vmonarch_paged_append", k, like, _tokens("k", k, like), _tokens("v", v, like), cache, _int32("q_starts", q_starts, like[2], (n,)), n - 1, nk, kv,
+         like[0],
          None if plan is None else byref(plan), at, nk)
 
 
 def paged_attention(q, cache_k, cache_v, table, q_starts, lengths, causal=True, scale=None, out=None, workspace=None):
     """Attention of each sequence's chunk of new tokens (q [tokens, heads_q, d], cut by q_starts) over its lengths[s] tokens in the pages, the chunk's
     own included.  Rows of no sequence are not written (see packed_attention)."""
-    nq, heads, d = _sizes("q", q)
+    nq, heads, like = _sizes("q", q)
+    d, _, dev = like
     n = q_starts.numel()
     if out is None:
         out = q.new_empty((nq, heads, d))
     else:
         _same_shape("out", out, q)
-    cache = _cache(cache_k, cache_v, table, lengths, q, n - 1)
+    cache = _cache(cache_k, cache_v, table, lengths, like, n - 1)
     kv = cache_k.shape[2]
     at, size = _workspace(workspace, q, "vmonarch_paged_attention_workspace_bytes", cache, n - 1, nq, heads, kv, d)
-    _run("vmonarch_paged_attention", q, _tokens("q", q, q), cache, _tokens("out", out, q), _int32("q_starts", q_starts, q, (n,)), n - 1, nq, heads, kv, d,
-         1.0 / math.sqrt(d) if scale is None else scale, 1 if causal else 0, None if at is None else at.data_ptr(), size)
+    _run("vmonarch_paged_attention", q, like, _tokens("q", q, like), cache, _tokens("out", out, like), _int32("q_starts", q_starts, dev, (n,)), n - 1, nq,
+         heads, kv, d, 1.0 / math.sqrt(d) if scale is None else scale, 1 if causal else 0, None if at is None else at.data_ptr(), size)
     return out

@@ -165,3 +165,9 @@ def test_counts_at_the_edge_of_32_bits():
     refuses(UNSUPPORTED, lib.vmonarch_paged_append(T(), T(1 << 18), wide, INT, 1, 8, 2, 64, None, None, 8, None), "room")
     plan = binding.rotary_plan([16])
     refuses(UNSUPPORTED, lib.vmonarch_rotary(T(), T(1 << 18), 1, None, None, 0, 2 ** 31 - 65535, 64, INT, 8, ctypes.byref(plan), 0, None), "tokens")
+
+
+def test_packed_descriptors_are_the_structures():
+    assert binding._pack_tokens(1 << 40, 3, 1 << 33) == bytes(Tokens(1 << 40, 3, 1 << 33))
+    values = (1 << 40, 1 << 41, 1, 2, 3, 4, 5, 1 << 33, 6, 7, 1 << 42, 1 << 34, 8, 1 << 43)
+    assert binding._pack_cache(*values) == bytes(Cache(*values))
