@@ -162,7 +162,7 @@ int vmonarch_paged_append_f32(const vmonarch_tokens* k, const vmonarch_tokens* v
 /*
  * Attention of each sequence's chunk of new tokens (or its single one) over its lengths[s] cached tokens, the chunk's own
  * included: vmonarch_packed_attention with the keys and values of sequence s taken from its pages.  Few rows over long caches are
- * cut into ranges of keys and joined by a second launch; the cut follows the sizes the host knows (tokens, n_seqs, heads, the longest
+ * cut into ranges of keys and joined by a second launch; the cut follows what the host knows (tokens, n_seqs, heads, the mask, the longest
  * sequence the table has room for), so the same sizes give the same bits.  workspace: DEVICE, 256-byte aligned, at least
  * vmonarch_paged_attention_workspace_bytes(...) bytes (0: none needed), or NULL for the process-wide one.
  */

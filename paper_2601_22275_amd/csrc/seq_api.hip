@@ -213,31 +213,40 @@ struct PagedPlan {
   bool few;
   int ranges;
 };
-PagedPlan paged_plan(long long table_keys, int n_seqs, long long tokens, int heads_kv, int group) {
+PagedPlan paged_plan(long long table_keys, int n_seqs, long long tokens, int heads_kv, int group, bool causal) {
   PagedPlan p;
   const long long rows = tokens * group;
   p.few = rows <= 32LL * n_seqs;
   const long long blocks = tile_bound(tokens, group, p.few ? 32 : 128, n_seqs) * heads_kv;
-  // Few rows: small workgroups that stream the cache, eight for every compute unit in turn (16 tokens over up to 16,384 keys: four 145 us, eight
-  // 136, sixteen 143).
-  // Many, two on a unit at once: as many ranges as one such round holds if those are three or more, else up to five, for four rounds, whose pieces of
-  // different length even out (chunks of up to 390 tokens over up to 8190, 12 heads, d = 128, us by ranges: 120 workgroups a range, 4 106, 5 128, 8
-  // 120; 180, 2 171, 5 148, 8 157; 290, 1 296, 2 177, 5 179, 8 191; 600, 1 325, 4 279, 8 312; 1200, 1 503, 2 454, 4 451, 8 536).  The pieces of one
-  // sequence are alike: as many ranges, up to five, as make rounds / ranges least, with what the partial results cost (over 8,190 to 32,768
-  // keys, us: 276 workgroups a range, 2 665, 3 501, 4 532, 5 473; 504, 1 366, 2 414, 5 445; 769, 1 1752, 2 1630, 3 1666, 5 1721).
   const long long shortest = p.few ? 256 : 512, slots = 2LL * compute_units();
-  long long r = 4 * slots;
-  if (!p.few && slots / blocks >= 3) r = slots / blocks;
-  else if (!p.few && n_seqs == 1) {
+  long long r = 1;
+  if (p.few) {
+    // Small workgroups that stream the cache, eight for every compute unit in turn (16 tokens over up to 16,384 keys: four 145 us, eight 136,
+    // sixteen 143).
+    r = (4 * slots + blocks - 1) / blocks;
+  } else if (slots / blocks >= 3) {
+    // Two on a unit at once: as many ranges as one such round holds (chunks of up to 390 tokens over up to 8190, 12 heads, d = 128, 120 workgroups a
+    // range, us: 3 102, 4 91, 5 106, 8 107).
+    r = slots / blocks;
+  } else {
+    // Up to five.  The unit of time is an uncut workgroup's.  Sequences of different length wait for the last piece, half of its length is for the
+    // balance to spare; the pieces of one sequence are alike and take whole rounds, unless it is short and causal.  A range's partial results cost
+    // what 350 keys do (us by ranges: 4 x up to 2048 causal tokens on up to 32,768 keys, 556 workgroups, 1 1272, 2 1129, 4 1066, 5 1071, 8 1109; one
+    // sequence: 2912 on 20,000, 276 workgroups, 1 511, 3 424, 4 440, 5 413; 5376 on 10,000, 504, 1 335, 2 358, 5 387; 8192 causal on 32,768, 768, 1
+    // 1621, 2 1448, 5 1498; 12,000 causal on themselves, 1128, 1 471, 2 528, 5 623).
+    const double each = (double)tokens / n_seqs, load = (double)blocks / slots;
+    const double keys = fmax(256.0, (n_seqs == 1 ? 1.0 : 0.5) * table_keys - (causal ? 0.5 * each : 0.0));
+    const bool alike = n_seqs == 1 && !(causal && 4 * tokens > table_keys);
     double least = 0;
     for (int x = 1; x <= 5; ++x) {
-      const double rounds = (double)((blocks * x + slots - 1) / slots) / x, partial = x == 1 ? 0 : (0.1 + 0.03 * x) * blocks / slots;
-      if (x == 1 || rounds + partial < least) {
-        least = rounds + partial;
+      const double time = (alike ? (double)((blocks * x + slots - 1) / slots) / x : n_seqs == 1 ? fmax(1.0 / x, load) : load + 1.0 / x) +
+                          (x > 1 ? load * 350 * x / keys : 0);
+      if (x == 1 || time < least) {
+        least = time;
         r = x;
       }
     }
-  } else r = p.few ? (r + blocks - 1) / blocks : r / blocks < 5 ? (r + blocks - 1) / blocks : 5;
+  }
   if (r > (table_keys + shortest - 1) / shortest) r = (table_keys + shortest - 1) / shortest;
   if (r < 1) r = 1;
   p.ranges = r > 64 ? 64 : (int)r;
@@ -387,7 +396,7 @@ int paged_impl(const vmonarch_tokens* q, const vmonarch_cache* cache, const vmon
   P.heads_kv = heads_kv; P.group = heads_q / heads_kv; P.d = d;
   P.causal = causal != 0; P.scale = scale;
   P.aligned = c.aligned && d % (16 / (int)sizeof(E)) == 0;
-  const PagedPlan plan = paged_plan((long long)cache->table_width * cache->page_size, n_seqs, tokens, heads_kv, P.group);
+  const PagedPlan plan = paged_plan((long long)cache->table_width * cache->page_size, n_seqs, tokens, heads_kv, P.group, causal != 0);
   P.ranges = plan.ranges;
   if (plan.ranges > 1) {
     const size_t need = vmonarch_paged_attention_workspace_bytes(cache, n_seqs, tokens, heads_q, heads_kv, d);
@@ -497,9 +506,13 @@ size_t vmonarch_paged_attention_workspace_bytes(const vmonarch_cache* cache, int
   if (cache == nullptr || cache->table_width < 1 || cache->page_size < 1 || n_seqs < 1 || tokens < 1 || heads_kv < 1 || heads_q < heads_kv ||
       heads_q % heads_kv != 0 || d < 1 || d > 256)
     return 0;
-  const PagedPlan plan = paged_plan((long long)cache->table_width * cache->page_size, n_seqs, tokens, heads_kv, heads_q / heads_kv);
-  if (plan.ranges < 2) return 0;
-  return ((size_t)plan.ranges * tokens * heads_q * (seq_padded(d) + 1) * sizeof(float) + 255) & ~(size_t)255;
+  int ranges = 1;  // with a causal mask or without
+  for (const bool causal : {false, true}) {
+    const int r = paged_plan((long long)cache->table_width * cache->page_size, n_seqs, tokens, heads_kv, heads_q / heads_kv, causal).ranges;
+    if (r > ranges) ranges = r;
+  }
+  if (ranges < 2) return 0;
+  return ((size_t)ranges * tokens * heads_q * (seq_padded(d) + 1) * sizeof(float) + 255) & ~(size_t)255;
 }
 int vmonarch_paged_attention(const vmonarch_tokens* q, const vmonarch_cache* cache, const vmonarch_tokens* out, const int32_t* q_starts, int n_seqs,
                              long long tokens, int heads_q, int heads_kv, int d, float scale, int causal, void* workspace, size_t workspace_bytes,
