@@ -516,3 +516,21 @@ def test_gradients_of_keys_that_many_rows_see(B, d, kv, group, ql, kl, causal):
         within(name, g[2:-1], tuple(x[2:-1] for x in want[name]))
     for x in (dk, dv):
         assert (x[:2] == 3).all() and (x[-1] == 3).all()
+
+
+CHUNKS = [
+    # many rows over caches long enough to be cut into ranges of keys; the last two: whole prompts
+    ("bf16", 128, 2, 1, [150, 1, 60], [3000, 900, 2100], 64, True, "page"),
+    ("bf16", 128, 1, 3, [129], [2600], 390, False, "head"),
+    ("bf16", 72, 2, 2, [90, 0, 40], [1500, 0, 1800], 39, True, "page"),
+    ("bf16", 64, 1, 1, [128], [2049], 3, True, "page"),
+    ("f32", 64, 1, 2, [60, 100], [1500, 100], 16, True, "page"),
+    ("bf16", 200, 1, 1, [70], [1300], 16, False, "page"),
+    ("bf16", 128, 2, 2, [700], [700], 16, True, "page"),
+    ("bf16", 64, 2, 1, [300, 512, 77], [300, 512, 77], 32, True, "page"),
+]
+
+
+@pytest.mark.parametrize("dtype,d,kv,group,new,have,page,causal,order", CHUNKS)
+def test_chunks_over_long_caches(B, dtype, d, kv, group, new, have, page, causal, order):
+    test_append_then_paged_attention(B, dtype, d, kv, group, new, have, page, causal, order)
