@@ -16,7 +16,7 @@
 // that where a row's weight sits on a few keys, so workgroups that see at most kSeqExactKeys keys sum D = sum_j P dP over them first.
 // Bound by the matrix units and the LDS reads that feed them (an operand per MFMA): they are busy for 0.4 of the cycles, the vector units for as
 // many, and two waves on a SIMD, all that the registers allow, overlap the two only in part.  3 x 4096 causal tokens, 12 heads on 4, d = 128: dQ
-// 209 us (868 TFLOP/s), dK and dV with their join 332 (728); forward and backward 653.  Operands requested further ahead, G and dP in turn, twice the rows
+// 214 us (849 TFLOP/s), dK and dV with their join 343 (705); forward and backward 643.  Operands requested further ahead, G and dP in turn, twice the rows
 // between barriers: level, or behind for spilled registers.
 #include "seq_device.h"
 

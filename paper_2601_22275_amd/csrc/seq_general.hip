@@ -11,7 +11,8 @@
 // The backward pass is two launches of one kernel, as the bf16 one: rows of queries own dq, rows of keys own dk and dv; the row sums
 // d_out . out come with the first and serve the second.
 // Bound by the matrix units (157 TFLOP/s in fp32; a large library product reaches 154) where rows are many, by the longest chain of tiles, 2 us each
-// at d = 128, where they are few.  4 ragged causal prompts of up to 1001 tokens, 10 heads on 2, d = 64, float32: 61 us (50 TFLOP/s).
+// at d = 128, where they are few.  4 ragged causal prompts of up to 1001 tokens, 10 heads on 2, d = 64, float32: 59 us (52 TFLOP/s); 9000 tokens 1181
+// (88; 1418 with the owner rows waited for in the loop and a branch per key group).
 #include <type_traits>
 
 #include "seq.h"

@@ -13,11 +13,13 @@
 // products of n - 1 dealt over the same instruction slots); the tiles at the end of the range that some row sees in part or
 // not at all (the diagonal, the ragged end) follow in plain order, with a true running maximum, masks, and a look at the values: zero times
 // infinity must not reach a row that does not see the key.
-// Bound by the matrix units and the LDS that feeds them (an operand per MFMA).  Two 32-row tiles per wave, which halve those reads and
-// leave one wave on a SIMD, measured level at 16,384 tokens (885 against 861 TFLOP/s at d = 128, 699 against 793 at d = 64) and behind on
-// everything shorter (16 x 1000 tokens, 12 heads, d = 128: 97 us against 68).  16,384 causal tokens, 12 heads on 4: 857 us at d = 128 (962
-// TFLOP/s; 900 us when it runs on and on: a large library product reaches 1233 here, both with the clock held down by power), 449 at d = 64 (918).  A lone workgroup
-// takes 0.9 us per 64 keys, which bounds short prompts (a dozen of up to 700 tokens: 19 us).
+// Bound by the matrix units, with the clock held down by power, where rows are many: 16,384 causal tokens, 12 heads on 4, 763 to 810 us at d =
+// 128 from card to card (1080 to 1018 TFLOP/s; a large library product reaches 1233), 433 to 446 at d = 64 (950).  The queries have to be waited for
+// in front of the loop: the compiler's own wait for them stood in it and took the tile just requested along (845 us in place of 763 on one card,
+// 107 in place of 87 for a frame over pages).  A lone workgroup takes 0.35 us per 32 keys at d = 64, 0.57 at 128, which bounds short prompts (a
+// dozen of up to 700 tokens: 17 us).  Level or behind: operands requested up to seven MFMAs ahead instead of three; keys and values requested three
+// and two tiles ahead and waited for by count; page addresses kept in scalar registers; two 32-row tiles per wave, which halve the LDS reads and
+// leave one wave on a SIMD (16 x 1000 tokens, 12 heads, d = 128: 97 us against 68).
 #include <type_traits>
 
 #include "seq_device.h"
@@ -104,8 +106,7 @@ __global__ void __launch_bounds__(64 * W2, 2) seq_attention_kernel(SeqParams<bf1
   const bf16_t* vbase = P.v.p + kvh * P.v.h + (PAGED ? 0LL : (long long)(k_begin + k0) * P.v.t);
   // Packed keys: a tile's address is wave-uniform, a lane's place in it a 32-bit offset (the host keeps a tile's rows within 2^31 bytes).
   // Pages: rows lie anywhere.  Their addresses are formed once each: every fourth tile each wave forms those of one of the next four (row_at), from
-  // entries of the table that came to LDS four tiles before (entry).  Sixty-four-bit products in every lane that loads cost 16,384 causal
-  // tokens 861 TFLOP/s in place of 947.
+  // entries of the table that came to LDS four tiles before (entry).  (Sixty-four-bit products in every lane that loads took 9 % of the rate.)
   const int row_k = (int)(2 * P.k.t), row_v = (int)(2 * P.v.t);  // bytes (packed keys)
   const int last_key = max(nk - 1, 0);
   auto key_of = [&](int t) __attribute__((always_inline)) { return min(k0 + t * BT + lane % BT, last_key); };
@@ -610,8 +611,8 @@ hipError_t launch_seq_attention_mfma(const SeqParams<bf16_t>& P, hipStream_t st)
   using rows64 = std::integral_constant<int, 64>;
   if constexpr (D == 64) {
     // Tiles of 64 keys while two workgroups a unit take the whole launch, tiles of 32 and three of them beyond (64 / 32, us: a dozen prompts of up to 700
-    // tokens, 12 heads on 4, 440 workgroups 20.9 / 23.9; 4 clips on 512 keys, 10 heads, 670 23.3 / 20.3; 16,384 causal tokens, 12 heads, 1536 485 /
-    // 453, 8192 without a mask 271 / 224).
+    // tokens, 12 heads on 4, 440 workgroups 19.1 / 20.0; 40 of them 39.8 / 33.4; 4 clips on 512 keys, 10 heads, 670 23.2 / 17.8; 16,384 causal tokens,
+    // 12 heads, 1536 454 / 446, 8192 without a mask 231 / 225).
     if (P.page_size > 0 && P.ranges > 1) return launch<D, 64, true, true, false>(P, st);
     return tile_bound(P.tokens_q, P.group, 32 * W2, P.n_seqs) * P.heads_kv > 2LL * compute_units() ? run(rows32{}) : run(rows64{});
   } else {

@@ -6,9 +6,9 @@
 // waves that take 32-key sub-tiles of its range in turn, each with LDS slots, a running maximum, a sum and accumulators of its own: no
 // barrier in the loop, a wave waits for its own loads only; two workgroups share a compute unit, so that one's start and end pass behind the
 // other's stream.  The waves join through LDS at the end, the ranges (blockIdx.y) through memory and a second launch.
-// 16 single tokens over up to 16,384 keys, 40 heads on 8, d = 128 (585 MB): 136 us, 4.3 TB/s with the join, where a large copy moves 5.0;
-// four waves in one workgroup 142, every lane forming the addresses of the rows it loads 160.  d = 64, 40 heads on 10 (366 MB): 90 us,
-// 4.1 TB/s; with four sub-tiles in LDS and two workgroups on a unit 110.  Products as in seq_mfma.hip: S^T = K Q^T and O^T += V^T P^T, both
+// 16 single tokens over up to 16,384 keys, 40 heads on 8, d = 128 (585 MB): 130 us, 4.5 TB/s with the join, where a large copy moves 5.0;
+// four waves in one workgroup 4 % more, every lane forming the addresses of the rows it loads 17 %, queries waited for in the loop 3 %.  d = 64, 40 heads on 10 (366 MB): 95 us,
+// 3.9 TB/s; with four sub-tiles in LDS and two workgroups on a unit 110.  Products as in seq_mfma.hip: S^T = K Q^T and O^T += V^T P^T, both
 // v_mfma_f32_32x32x16_bf16.
 #include "seq_device.h"
 
