@@ -55,9 +55,6 @@ struct SeqParams {
   int ranges;
 };
 
-// Backward, bf16: rows of queries whose workgroup sees at most this many keys sum D over them instead of reading it off the stored output
-constexpr int kSeqExactKeys = 512;
-
 // ---- device: sequences --------------------------------------------------------------------------------------------------------
 struct Span {
   int seq, tile;     // tile of `BM` packed rows (keys: group 1) within the sequence

@@ -11,9 +11,14 @@
 //   G^T = X1 R1^T, dP^T = X2 R2^T       lane (i, g) holds owner row i against 16 of 32 stream rows
 //   P = 2^(G scale log2 e - lse log2 e),  dS = P (dP - D)
 //   acc^T += Xa^T E                     E = dS or P, converted to bf16 where it stands; Xa^T by LDS transpose reads
-// (seven products where five would do with dQ accumulated in memory by atomics.)  The dQ launch forms D = d_out . out from the rows it
-// holds and leaves {lse log2 e, D} per packed row to the other.  D read off the stored out carries its rounding; dP - D does not forgive
-// that where a row's weight sits on a few keys, so workgroups that see at most kSeqExactKeys keys sum D = sum_j P dP over them first.
+// (seven products where five would do with dQ accumulated in memory by atomics.)  The dQ launch leaves {lse log2 e, D} per packed row to the
+// other.  D = sum_j P dP is known after the last key only; D' = d_out . out from the stored rows carries the rounding of out, which dP - D does
+// not forgive where a row's weight sits on a few keys.  So the launch forms dS' = P (dP - D') and corrects both at the end, with sum_j P = 1:
+//   D = D' + sum_j dS'        dq / scale = sum_j dS' k - (sum_j dS') sum_j P k
+// at the cost of an eighth product, sum_j P k, on the operands of the first (3 x 4096 tokens forward and backward 652 -> 711 us; D summed in a round of its
+// own would be two products).  For dq the sum is of the ROUNDED dS': the weights that the keys really
+// get add up to zero, so a row that sits on one key loses no digits to it, nor does what all keys have in common.  Errors of dq and dk stay at 1.2 to
+// 1.5 roundings of the result at any sharpness and length (with D' alone 2.7 to 4.4 at logit deviations of 8 and 16).
 // Bound by the matrix units and the LDS reads that feed them (an operand per MFMA): they are busy for 0.4 of the cycles, the vector units for as
 // many, and two waves on a SIMD, all that the registers allow, overlap the two only in part.  3 x 4096 causal tokens, 12 heads on 4, d = 128: dQ
 // 214 us (849 TFLOP/s), dK and dV with their join 343 (705); forward and backward 643.  Operands requested further ahead, G and dP in turn, twice the rows
@@ -37,10 +42,10 @@ template <int D, int MODE>
 constexpr int tile_rows() {  // stream rows per LDS tile
   return (D == 128 ? 8 : 16) * waves<MODE>();
 }
-// k-steps of the second owner tensor that wait in LDS: the dK, dV launch at d = 128 just fills a wave's 256 registers
-template <int D, int MODE>
+// k-steps of the second owner tensor that wait in LDS: at d = 128 two sets of accumulators just fill a wave's 256 registers
+template <int D>
 constexpr int own_in_lds() {
-  return D == 128 && MODE == DKV ? 4 : 0;
+  return D == 128 ? 4 : 0;
 }
 
 template <int D, int MODE>
@@ -58,10 +63,11 @@ __global__ void __launch_bounds__(64 * waves<MODE>(), 2) seq_bwd_kernel(SeqParam
   constexpr int NST = MODE == DKV ? 2 : 0;  // arrays of stream statistics: lse log2 e, D
   constexpr int STATS_OFF = NSLOT * SLOT_BYTES;
   constexpr int STATS_SLOT = NST * SR * 4;
-  constexpr int NACC = MODE == DKV ? 2 : 1;
-  constexpr bool TIGHT = MODE == DKV && D == 128;
+  constexpr int NACC = 2;                  // E = dS, and E = P
+  constexpr int NX = MODE == DKV ? 2 : 1;  // dK, dV: their operands are of two tensors (queries, d_out); dQ: of one (keys)
+  constexpr bool TIGHT = D == 128;
   constexpr int NG = 2 * KS;
-  constexpr int NL = own_in_lds<D, MODE>();
+  constexpr int NL = own_in_lds<D>();
   constexpr int OWN_OFF = STATS_OFF + NSLOT * STATS_SLOT;
   auto swz = [](int row) { return G::swz(row); };
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -215,7 +221,9 @@ __global__ void __launch_bounds__(64 * waves<MODE>(), 2) seq_bwd_kernel(SeqParam
   const unsigned own_base = lds_base + OWN_OFF + (ot * NL * 64 + lane) * 16;  // (written alike by the waves that share it)
   const int otok = MODE == DKV ? 0 : orow / group, ohead = orow - otok * group;
   const bf16x8 zero8 = {0, 0, 0, 0, 0, 0, 0, 0};
+  float o_l2 = 0.f, o_delta = 0.f;  // of the owner row where it is a query: lse log2 e, D'
   {
+    const bf16_t* op = P.o.p + (long long)(q_begin + otok) * P.o.t + (long long)(kvh * group + ohead) * P.o.h + 8 * g;
     const bf16_t* r1 = MODE == DKV ? kbase + (long long)orow * P.k.t : qbase + (long long)otok * P.q.t + ohead * P.q.h;
     const bf16_t* r2 = MODE == DKV ? vbase + (long long)orow * P.v.t : dobase + (long long)otok * P.d_out.t + ohead * P.d_out.h;
 #pragma unroll
@@ -225,22 +233,16 @@ __global__ void __launch_bounds__(64 * waves<MODE>(), 2) seq_bwd_kernel(SeqParam
       const bf16x8 x = in ? *reinterpret_cast<const bf16x8*>(r2 + 8 * g + 16 * ks) : zero8;
       if (ks < KS - NL) reg2[ks] = x;
       else *(lds_b128_wptr)(unsigned long long)(own_base + (ks - (KS - NL)) * 1024) = x;
+      if (MODE == DQ) {
+        const bf16x8 y = in ? *reinterpret_cast<const bf16x8*>(op + 16 * ks) : zero8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o_delta = __builtin_fmaf((float)x[i], (float)y[i], o_delta);
+      }
     }
   }
   const float sc2 = P.scale * LOG2E;
-  const bool exact = MODE == DQ && s1 <= kSeqExactKeys;
-  float o_l2 = 0.f, o_delta = 0.f;  // of the owner row where it is a query
   if (MODE == DQ) {
-    if (!exact) {
-      const bf16_t* op = P.o.p + (long long)(q_begin + otok) * P.o.t + (long long)(kvh * group + ohead) * P.o.h + 8 * g;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8 x = 16 * ks + 8 * g < P.d ? *reinterpret_cast<const bf16x8*>(op + 16 * ks) : zero8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o_delta = __builtin_fmaf((float)x[i], (float)reg2[MODE == DQ ? ks : 0][i], o_delta);
-      }
-      o_delta += __shfl_xor(o_delta, 32);
-    }
+    o_delta += __shfl_xor(o_delta, 32);
     o_l2 = P.lse[(long long)(kvh * group + ohead) * P.tokens_q + q_begin + otok] * LOG2E;
     if (o_l2 == -INFINITY) o_l2 = INFINITY;  // a row that sees nothing: no weight anywhere
   }
@@ -274,8 +276,8 @@ __global__ void __launch_bounds__(64 * waves<MODE>(), 2) seq_bwd_kernel(SeqParam
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[x][ct][r] = 0.f;
-  float d_sum = 0.f;
-  constexpr int NOP = NG + 2 * CT * NACC;  // MFMAs of a sub-tile: G, dP, then the products
+  float d_sum = 0.f, e_sum = 0.f;  // dQ: dS' of the owner row summed before and after its rounding
+  constexpr int NOP = NG + 2 * CT * NX;  // operands of a sub-tile: of G, dP, then of the products
   constexpr int PF = TIGHT ? 2 : 3;
   const bool active = o0 + ot * 32 < owners;
   // stream rows that every owner row of the wave goes with lie in whole_lo .. whole_hi - 1
@@ -283,12 +285,14 @@ __global__ void __launch_bounds__(64 * waves<MODE>(), 2) seq_bwd_kernel(SeqParam
   range_of(min(o0 + ot * 32 + 31, owners - 1), &whole_lo, &unused);
   range_of(min(o0 + ot * 32, owners - 1), &unused, &whole_hi);
 
-  // ---- one 32-row sub-tile of the stream; SUM: only the owner's sum of P dP -------------------------------------------------------------
-  auto step = [&](unsigned slot, unsigned sslot, auto st_c, auto sum_c, int first) __attribute__((always_inline)) {
+  typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+  bf16x2 ones2;
+  ones2[0] = (__bf16)1.0f;
+  ones2[1] = (__bf16)1.0f;
+  // ---- one 32-row sub-tile of the stream ------------------------------------------------------------------------------------------------
+  auto step = [&](unsigned slot, unsigned sslot, auto st_c, int first) __attribute__((always_inline)) {
     constexpr int ST = decltype(st_c)::value;
-    constexpr bool SUM = decltype(sum_c)::value;
     constexpr int SUB = ST * 32 * ROW_BYTES;
-    constexpr int LAST = SUM ? NG : NOP;
     f32x16 s, dp;
 #pragma unroll
     for (int r = 0; r < 16; ++r) { s[r] = 0.f; dp[r] = 0.f; }
@@ -304,8 +308,8 @@ __global__ void __launch_bounds__(64 * waves<MODE>(), 2) seq_bwd_kernel(SeqParam
       } else if constexpr (I < NG) {
         ring[I & 3] = rd_row((ab ^ ((I - KS) << 5)) + SUB + TILE_BYTES);
         if constexpr (I >= NG - NL) own[I - (NG - NL)] = rd_row(own_base + (I - (NG - NL)) * 1024);
-      } else if constexpr (I < LAST) {
-        constexpr int c = (I - NG) / (CT * NACC), ct = (I - NG) / NACC % CT, x = (NACC - 1) - (I - NG) % NACC;  // dV first: P is there before dS
+      } else if constexpr (I < NOP) {
+        constexpr int c = (I - NG) / (CT * NX), ct = (I - NG) / NX % CT, x = (NX - 1) - (I - NG) % NX;  // dV first: P is there before dS
         constexpr int off = SUB + c * 16 * ROW_BYTES + (x == 1 ? TILE_BYTES : 0);
         ring[I & 3] = rd_tr((tb0 ^ (ct << 6)) + off, (tb1 ^ (ct << 6)) + off);
       }
@@ -344,30 +348,35 @@ __global__ void __launch_bounds__(64 * waves<MODE>(), 2) seq_bwd_kernel(SeqParam
     auto score = [&](auto rc) __attribute__((always_inline)) {
       constexpr int r = decltype(rc)::value;
       const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], sc2, -l2[r & 3]));
-      if (SUM) {
-        d_sum = __builtin_fmaf(p, dp[r], d_sum);
-      } else {
-        if (MODE == DKV) pb[r >> 3][r & 7] = (__bf16)p;
-        eb[r >> 3][r & 7] = (__bf16)(p * (dp[r] - dd[r & 3]));
+      const float e = p * (dp[r] - dd[r & 3]);
+      pb[r >> 3][r & 7] = (__bf16)p;
+      eb[r >> 3][r & 7] = (__bf16)e;
+      if (MODE == DQ) {
+        d_sum += e;
+        if constexpr (r & 1) {
+          bf16x2 two;
+          two[0] = eb[r >> 3][(r & 7) - 1];
+          two[1] = eb[r >> 3][r & 7];
+          e_sum = __builtin_amdgcn_fdot2_f32_bf16(two, ones2, e_sum, false);
+        }
       }
     };
     // The first 16 rows' scores, then the other 16's between the products of the first
-    constexpr int FIRST = SUM ? 4 : 2;
-    static_for<0, FIRST>([&](auto r4_c) __attribute__((always_inline)) {
+    static_for<0, 2>([&](auto r4_c) __attribute__((always_inline)) {
       constexpr int r4 = decltype(r4_c)::value;
       stats(r4_c);
       static_for<4 * r4, 4 * r4 + 4>(score);
       if (TIGHT) __builtin_amdgcn_sched_barrier(0);
     });
     __builtin_amdgcn_sched_barrier(0);
-    static_for<NG, LAST>([&](auto ic) __attribute__((always_inline)) {
+    static_for<NG, NOP>([&](auto ic) __attribute__((always_inline)) {
       constexpr int I = decltype(ic)::value;
-      constexpr int c = (I - NG) / (CT * NACC), ct = (I - NG) / NACC % CT, x = (NACC - 1) - (I - NG) % NACC;
+      constexpr int c = (I - NG) / (CT * NX), ct = (I - NG) / NX % CT, x = (NX - 1) - (I - NG) % NX;
       request(std::integral_constant<int, I + PF>{});
-      if constexpr (x == 1) acc[x][ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[I & 3], pb[c], acc[x][ct], 0, 0, 0);
-      else acc[x][ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[I & 3], eb[c], acc[0][ct], 0, 0, 0);
+      if constexpr (MODE == DQ || x == 1) acc[1][ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[I & 3], pb[c], acc[1][ct], 0, 0, 0);
+      if constexpr (MODE == DQ || x == 0) acc[0][ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[I & 3], eb[c], acc[0][ct], 0, 0, 0);
       if constexpr (c == 0) {
-        constexpr int PER = 8 / (CT * NACC), r0 = 8 + PER * (I - NG);
+        constexpr int PER = 8 / (CT * NX), r0 = 8 + PER * (I - NG);
         static_for<r0, r0 + PER>([&](auto rc) __attribute__((always_inline)) {
           if constexpr (decltype(rc)::value % 4 == 0) stats(std::integral_constant<int, decltype(rc)::value / 4>{});
           score(rc);
@@ -379,35 +388,31 @@ __global__ void __launch_bounds__(64 * waves<MODE>(), 2) seq_bwd_kernel(SeqParam
 
   // Tile t sits in slot t mod 3 and is requested two iterations ahead; the barrier at the top of iteration t publishes it and retires
   // tile t - 1, whose slot tile t + 2 takes.
-  auto stream = [&](auto sum_c) __attribute__((always_inline)) {
-    for (int t = 0; t < ntiles; ++t) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (t + 2 < ntiles) issue_tile(t + 2);
-      if (active) {
-        constexpr int MINE = BK / SHARE;  // rows of a tile that are this wave's
-        const unsigned slot = (t % NSLOT) * SLOT_BYTES + part_of * (MINE * ROW_BYTES);
-        const unsigned sslot = lds_base + STATS_OFF + (t % NSLOT) * STATS_SLOT + 16 * g + part_of * (MINE * 4);
-        const int first = s0 + t * BK + part_of * MINE;
-        step(slot, sslot, std::integral_constant<int, 0>{}, sum_c, first);
-        if constexpr (MINE == 64) step(slot, sslot, std::integral_constant<int, 1>{}, sum_c, first + 32);
-      }
-    }
-  };
-  if (MODE == DQ) {
-    if (exact) {
-      stream(std::true_type{});
-      o_delta = d_sum + __shfl_xor(d_sum, 32);
-      __syncthreads();  // everyone is done with the tiles
-      if (ntiles > 0) issue_tile(0);
-      if (ntiles > 1) issue_tile(1);
-    }
-    if (ovalid && g == 0) {
-      stat_l[orow] = o_l2;
-      stat_d[orow] = o_delta;
+  for (int t = 0; t < ntiles; ++t) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (t + 2 < ntiles) issue_tile(t + 2);
+    if (active) {
+      constexpr int MINE = BK / SHARE;  // rows of a tile that are this wave's
+      const unsigned slot = (t % NSLOT) * SLOT_BYTES + part_of * (MINE * ROW_BYTES);
+      const unsigned sslot = lds_base + STATS_OFF + (t % NSLOT) * STATS_SLOT + 16 * g + part_of * (MINE * 4);
+      const int first = s0 + t * BK + part_of * MINE;
+      step(slot, sslot, std::integral_constant<int, 0>{}, first);
+      if constexpr (MINE == 64) step(slot, sslot, std::integral_constant<int, 1>{}, first + 32);
     }
   }
-  stream(std::false_type{});
+  if (MODE == DQ) {
+    d_sum += __shfl_xor(d_sum, 32);
+    e_sum += __shfl_xor(e_sum, 32);
+    if (ovalid && g == 0) {
+      stat_l[orow] = o_l2;
+      stat_d[orow] = o_delta + d_sum;
+    }
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[0][ct][r] = __builtin_fmaf(-e_sum, acc[1][ct][r], acc[0][ct][r]);
+  }
 
   __syncthreads();
   int tid_e = threadIdx.x;
@@ -465,7 +470,7 @@ __global__ void __launch_bounds__(64 * waves<MODE>(), 2) seq_bwd_kernel(SeqParam
   char* stage = smem + ot * (32 * ROW_BYTES);
   static_assert(NT * 32 * ROW_BYTES <= NSLOT * SLOT_BYTES, "staged rows fit the tile slots");
 #pragma unroll
-  for (int x = 0; x < NACC; ++x) {
+  for (int x = 0; x < NX; ++x) {
     const float f = x == 1 ? 1.0f : P.scale;
     const Rows<bf16_t>& dst = MODE == DQ ? P.dq : x == 1 ? P.dv : P.dk;
 #pragma unroll
@@ -513,7 +518,7 @@ __global__ void __launch_bounds__(256) seq_bwd_join_kernel(SeqParams<bf16_t> P) 
 
 template <int D, int MODE>
 hipError_t launch(const SeqParams<bf16_t>& P, hipStream_t st) {
-  constexpr int LDS = 2 * NSLOT * tile_rows<D, MODE>() * D * 2 + (MODE == DKV ? NSLOT * 2 * tile_rows<D, MODE>() * 4 : 0) + NT * own_in_lds<D, MODE>() * 1024;
+  constexpr int LDS = 2 * NSLOT * tile_rows<D, MODE>() * D * 2 + (MODE == DKV ? NSLOT * 2 * tile_rows<D, MODE>() * 4 : 0) + NT * own_in_lds<D>() * 1024;
   const long long tiles = MODE == DKV ? tile_bound(P.tokens_k, 1, 32 * NT, P.n_seqs) : tile_bound(P.tokens_q, P.group, 32 * NT, P.n_seqs);
   if (tiles * P.heads_kv > 0x7fffffffLL) return hipErrorInvalidValue;
   auto kern = seq_bwd_kernel<D, MODE>;

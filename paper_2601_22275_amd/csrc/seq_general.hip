@@ -96,6 +96,9 @@ __global__ void __launch_bounds__(256 * parts<D>(), D == 256 ? 1 : 2) seq_genera
   constexpr int NJ = D / 16;         // 16-channel groups of a contraction over channels
   constexpr int NC = D / 64;         // 64-channel groups of an output row
   constexpr bool BWD = MODE != FORWARD;
+  // d_out . out from stored rows of bf16 carries their rounding, which the difference dP - D does not forgive where a row's weight sits on a few keys
+  // (on one: dP - D is zero): D = sum_j P dP in a round of its own.
+  constexpr bool SUM_D = MODE == GRAD_Q && sizeof(E) == 2;
   constexpr int PARTS = parts<D>();
   __shared__ __attribute__((aligned(16))) float tiles_lds[PARTS][2][BN][LS];
   __shared__ float st_lds[PARTS][2][MODE == GRAD_KV ? BN : 1];
@@ -162,15 +165,17 @@ __global__ void __launch_bounds__(256 * parts<D>(), D == 256 ? 1 : 2) seq_genera
   if (MODE != GRAD_KV) {
     limit = !ovalid ? 0 : P.causal ? min(max(more + 1 + (int)(orow / group), 0), nk) : nk;
     if (MODE == GRAD_Q) {
-      const E* po = q_row(P.o, ovalid ? orow : owners - 1);
+      if (!SUM_D) {
+        const E* po = q_row(P.o, ovalid ? orow : owners - 1);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const f32x4 o = load4<E>(po, 16 * j + 4 * g, d, al);
+        for (int j = 0; j < NJ; ++j) {
+          const f32x4 o = load4<E>(po, 16 * j + 4 * g, d, al);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o_delta = __builtin_fmaf(o[e], r2[BWD ? j : 0][e], o_delta);
+          for (int e = 0; e < 4; ++e) o_delta = __builtin_fmaf(o[e], r2[BWD ? j : 0][e], o_delta);
+        }
+        o_delta += __shfl_xor(o_delta, 16);
+        o_delta += __shfl_xor(o_delta, 32);
       }
-      o_delta += __shfl_xor(o_delta, 16);
-      o_delta += __shfl_xor(o_delta, 32);
       if (ovalid) {
         const long long at = stat_of(orow);
         o_lse = P.lse[at] * LOG2E;
@@ -225,11 +230,7 @@ __global__ void __launch_bounds__(256 * parts<D>(), D == 256 ? 1 : 2) seq_genera
       for (int ct = 0; ct < 4; ++ct) acc[x][c][ct] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
 
-  // d_out . out from the stored rows carries their rounding, which the difference dP - D does not forgive where a row's weight sits on a few
-  // keys (on one: dP - D is zero).  Rows of bf16 that see few keys get D = sum_j P dP in a round of its own.
-  const bool exact = MODE == GRAD_Q && sizeof(E) == 2 && s1 <= kSeqExactKeys;
-  for (int round = exact ? 0 : 1; round < 2; ++round) {
-  if (MODE == GRAD_Q && exact && round == 0) o_delta = 0.f;
+  for (int round = SUM_D ? 0 : 1; round < 2; ++round) {
   float d_sum = 0.f;
   // (past the last tile the half that has none left multiplies zeros)
   if (ntiles > 0) fetch(part);
