@@ -21,6 +21,9 @@
  *   - bf16 with d <= 128, d a multiple of 8, rows on 16-byte boundaries (and packed keys less than 2^24 elements apart)
  *     runs on the bf16 matrix units; everything else on the fp32 matrix units, with the same results to the tensors'
  *     precision.  Values beyond 2^98 may overflow in sums that would not overflow as weights of at most 1.
+ *   - Logits are formed in fp32, so a weight is off by 2^-24 of its logit's magnitude, relatively; in gradients twice, the log-sum-exp is one too.  The
+ *     bf16 matrix units take finite logits of up to 2^28 in magnitude (beyond, the rounding of a row's reference alone can carry its weights out of
+ *     fp32's range: the row may come out as zeros or not finite), the fp32 ones any that fp32 holds.
  *   - Results do not depend on the order in which workgroups run: nothing is accumulated across them by atomics.
  */
 #ifndef VMONARCH_SEQUENCE_H_

@@ -10,7 +10,7 @@ namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
-constexpr float NEG_BIG = -1.0e30f;  // the reference of a row that has seen nothing: finite, so that -inf - reference is -inf
+constexpr float NEG_BIG = -3.402823466e38f;  // the reference of a row that has seen nothing: below any finite logit, and finite, so that -inf - reference is -inf
 
 template <int I, int N, typename F>
 __device__ __forceinline__ void static_for(F&& f) {
