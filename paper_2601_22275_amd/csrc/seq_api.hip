@@ -339,7 +339,7 @@ int packed_bwd_impl(const vmonarch_tokens* q, const vmonarch_tokens* k, const vm
   if (rc) return rc;
   for (const auto& a : all)
     for (const auto& b : all)
-      if (a.output && a.x != b.x && a.x->data == b.x->data && a.x->data != nullptr)
+      if (a.output && &a != &b && a.x->data == b.x->data && a.x->data != nullptr)
         return api_fail(VMONARCH_ERR_INVALID_ARG, "%s must not be %s", a.what, b.what);
   if (dq == dk || dq == dv || dk == dv) return api_fail(VMONARCH_ERR_INVALID_ARG, "dq, dk and dv must differ");
   if (tokens_q > 0 && lse == nullptr) return api_fail(VMONARCH_ERR_INVALID_ARG, "null lse");
