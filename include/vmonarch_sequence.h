@@ -110,10 +110,12 @@ int vmonarch_packed_attention_f32(const vmonarch_tokens* q, const vmonarch_token
  *   dq[i] = scale sum_j dS[i,j] k[j]     dk[j] = scale sum_i dS[i,j] q[i]     dv[j] = sum_i P[i,j] d_out[i],
  * dk and dv summed over the query heads that share a key head.  out and lse as the forward pass left them.  Rows of dk and dv that
  * no query sees are set to zero.  workspace: DEVICE, 256-byte aligned, at least
- * vmonarch_packed_attention_bwd_workspace_bytes(...) bytes for the call's sizes (0 on invalid ones, and without queries), or NULL for the
- * process-wide one.
+ * vmonarch_packed_attention_bwd_workspace_bytes(...) bytes for the call's type and sizes (0 on invalid ones, and without queries), or NULL for the
+ * process-wide one.  (bf16: partial gradients of keys that many rows see are among them; float32, and bf16 that the bf16 matrix units do not take, need two
+ * floats a row.)
  */
 size_t vmonarch_packed_attention_bwd_workspace_bytes(int n_seqs, long long tokens_q, long long tokens_k, int heads_q, int heads_kv, int d);
+size_t vmonarch_packed_attention_bwd_workspace_bytes_f32(int n_seqs, long long tokens_q, long long tokens_k, int heads_q, int heads_kv, int d);
 int vmonarch_packed_attention_bwd(const vmonarch_tokens* q, const vmonarch_tokens* k, const vmonarch_tokens* v,
                                   const vmonarch_tokens* out, const vmonarch_tokens* d_out, const float* lse,
                                   const vmonarch_tokens* dq, const vmonarch_tokens* dk, const vmonarch_tokens* dv,

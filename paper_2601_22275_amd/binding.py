@@ -40,6 +40,7 @@ EXPORTS = [
     "vmonarch_recompute_tokens", "vmonarch_recompute_tokens_f32",
     "vmonarch_rotary_init", "vmonarch_rotary_scale", "vmonarch_rotary", "vmonarch_rotary_f32",
     "vmonarch_packed_attention", "vmonarch_packed_attention_f32", "vmonarch_packed_attention_bwd_workspace_bytes",
+    "vmonarch_packed_attention_bwd_workspace_bytes_f32",
     "vmonarch_packed_attention_bwd", "vmonarch_packed_attention_bwd_f32", "vmonarch_paged_append", "vmonarch_paged_append_f32",
     "vmonarch_paged_attention_workspace_bytes", "vmonarch_paged_attention", "vmonarch_paged_attention_f32",
 ]
@@ -141,11 +142,11 @@ def lib() -> ctypes.CDLL:
             getattr(L, "vmonarch_packed_attention" + suffix).argtypes = [c_void_p] * 7 + [c_int, n, n, c_int, c_int, c_int, c_float, c_int, c_void_p]
             getattr(L, "vmonarch_packed_attention_bwd" + suffix).argtypes = [c_void_p] * 11 + [c_int, n, n, c_int, c_int, c_int, c_float, c_int,
                                                                                               c_void_p, c_size_t, c_void_p]
+            size = getattr(L, "vmonarch_packed_attention_bwd_workspace_bytes" + suffix)
+            size.restype, size.argtypes = c_size_t, [c_int, n, n, c_int, c_int, c_int]
             getattr(L, "vmonarch_paged_append" + suffix).argtypes = [c_void_p] * 4 + [c_int, n, c_int, c_int, c_void_p, c_void_p, n, c_void_p]
             getattr(L, "vmonarch_paged_attention" + suffix).argtypes = [c_void_p] * 4 + [c_int, n, c_int, c_int, c_int, c_float, c_int, c_void_p,
                                                                                         c_size_t, c_void_p]
-        L.vmonarch_packed_attention_bwd_workspace_bytes.restype = c_size_t
-        L.vmonarch_packed_attention_bwd_workspace_bytes.argtypes = [c_int, n, n, c_int, c_int, c_int]
         L.vmonarch_paged_attention_workspace_bytes.restype = c_size_t
         L.vmonarch_paged_attention_workspace_bytes.argtypes = [c_void_p, c_int, n, c_int, c_int, c_int]
         _lib = L
@@ -550,7 +551,7 @@ def packed_attention_bwd(q, k, v, out, d_out, lse, q_starts, k_starts=None, caus
     n = q_starts.numel()
     qs = _int32("q_starts", q_starts, dev, (n,))
     ks = qs if k_starts is None or k_starts is q_starts else _int32("k_starts", k_starts, dev, (n,))
-    at, size = _workspace(workspace, q, "vmonarch_packed_attention_bwd_workspace_bytes", n - 1, nq, nk, heads, kv, d)
+    at, size = _workspace(workspace, q, "vmonarch_packed_attention_bwd_workspace_bytes" + _suffix(q), n - 1, nq, nk, heads, kv, d)
     _run("vmonarch_packed_attention_bwd", q, like, _tokens("q", q, like), _tokens("k", k, like), _tokens("v", v, like), _tokens("out", out, like),
          _tokens("d_out", d_out, like), lse.data_ptr(), _tokens("dq", dq, like), _tokens("dk", dk, like), _tokens("dv", dv, like), qs, ks, n - 1, nq, nk,
          heads, kv, d, 1.0 / math.sqrt(d) if scale is None else scale, 1 if causal else 0, None if at is None else at.data_ptr(), size)

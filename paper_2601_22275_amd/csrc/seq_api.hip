@@ -270,10 +270,16 @@ hipError_t launch_attention(const SeqParams<E>& P, bool few, hipStream_t st) {
   return e == hipSuccess && P.ranges > 1 ? launch_seq_join<E>(P, st) : e;
 }
 
+// Whether the bf16 matrix units take a backward pass: seq_bwd.hip, else seq_general.hip
+template <typename E>
+bool bwd_on_bf16_units(bool aligned, int d) {
+  return sizeof(E) == 2 && aligned && d <= 128;
+}
+
 template <typename E>
 hipError_t launch_attention_bwd(const SeqParams<E>& P, hipStream_t st) {
   if constexpr (sizeof(E) == 2) {
-    if (P.aligned && P.d <= 128) return P.d <= 64 ? launch_seq_bwd_mfma<64>(P, st) : launch_seq_bwd_mfma<128>(P, st);
+    if (bwd_on_bf16_units<E>(P.aligned, P.d)) return P.d <= 64 ? launch_seq_bwd_mfma<64>(P, st) : launch_seq_bwd_mfma<128>(P, st);
   }
   return launch_seq_attention_bwd_general<E>(P, st);
 }
@@ -307,18 +313,25 @@ int packed_impl(const vmonarch_tokens* q, const vmonarch_tokens* k, const vmonar
   return hip_result(launch_attention<E>(P, false, as_stream(stream)), "packed_attention launch");
 }
 
-// Workspace of the backward pass: two statistics per query row, then the partial dK and dV of the ranges of rows
+// Workspace of the backward pass: two statistics per query row, then (bf16 matrix units) the partial dK and dV of the ranges of rows
 struct BwdLayout {
   size_t parts, total;
   int ranges;
 };
-BwdLayout bwd_layout(int n_seqs, long long tokens_q, long long tokens_k, int heads_q, int heads_kv, int d) {
+BwdLayout bwd_layout(bool bf16_units, int n_seqs, long long tokens_q, long long tokens_k, int heads_q, int heads_kv, int d) {
   BwdLayout l;
-  l.ranges = d <= 128 ? seq_bwd_ranges(n_seqs, tokens_q, tokens_k, heads_kv, heads_q / heads_kv) : 1;
+  l.ranges = bf16_units ? seq_bwd_ranges(n_seqs, tokens_q, tokens_k, heads_kv, heads_q / heads_kv) : 1;
   l.parts = ((size_t)tokens_q * heads_q * 2 * sizeof(float) + 255) & ~(size_t)255;
   l.total = l.parts;
   if (l.ranges > 1) l.total += ((size_t)l.ranges * 2 * tokens_k * heads_kv * seq_padded(d) * sizeof(float) + 255) & ~(size_t)255;
   return l;
+}
+
+// (rows taken to be aligned: less is needed where they are not)
+template <typename E>
+size_t bwd_workspace(int n_seqs, long long tokens_q, long long tokens_k, int heads_q, int heads_kv, int d) {
+  if (n_seqs < 1 || tokens_q < 1 || tokens_k < 0 || heads_kv < 1 || heads_q < heads_kv || heads_q % heads_kv != 0 || d < 1 || d > 256) return 0;
+  return bwd_layout(bwd_on_bf16_units<E>(d % (16 / (int)sizeof(E)) == 0, d), n_seqs, tokens_q, tokens_k, heads_q, heads_kv, d).total;
 }
 
 template <typename E>
@@ -349,9 +362,10 @@ int packed_bwd_impl(const vmonarch_tokens* q, const vmonarch_tokens* k, const vm
     return api_fail(VMONARCH_ERR_INVALID_ARG, "workspace and workspace_bytes must both be zero or both non-zero");
   if (tokens_q == 0 && tokens_k == 0) return VMONARCH_OK;
   SeqParams<E> P = {};
+  P.aligned = c.aligned && d % (16 / (int)sizeof(E)) == 0;
   P.ranges = 1;
   if (tokens_q > 0) {
-    const BwdLayout l = bwd_layout(n_seqs, tokens_q, tokens_k, heads_q, heads_kv, d);
+    const BwdLayout l = bwd_layout(bwd_on_bf16_units<E>(P.aligned, d), n_seqs, tokens_q, tokens_k, heads_q, heads_kv, d);
     char* ws = (char*)api_workspace(l.total, &rc, workspace, workspace_bytes, as_stream(stream));
     if (rc) return rc;
     P.delta = (float*)ws;
@@ -365,7 +379,6 @@ int packed_bwd_impl(const vmonarch_tokens* q, const vmonarch_tokens* k, const vm
   P.tokens_q = (int)tokens_q; P.tokens_k = (int)tokens_k;
   P.heads_kv = heads_kv; P.group = heads_q / heads_kv; P.d = d;
   P.causal = causal != 0; P.scale = scale;
-  P.aligned = c.aligned && d % (16 / (int)sizeof(E)) == 0;
   return hip_result(launch_attention_bwd<E>(P, as_stream(stream)), "packed_attention_bwd launch");
 }
 
@@ -471,8 +484,10 @@ int vmonarch_packed_attention_f32(const vmonarch_tokens* q, const vmonarch_token
 }
 
 size_t vmonarch_packed_attention_bwd_workspace_bytes(int n_seqs, long long tokens_q, long long tokens_k, int heads_q, int heads_kv, int d) {
-  if (n_seqs < 1 || tokens_q < 1 || tokens_k < 0 || heads_kv < 1 || heads_q < heads_kv || heads_q % heads_kv != 0 || d < 1 || d > 256) return 0;
-  return bwd_layout(n_seqs, tokens_q, tokens_k, heads_q, heads_kv, d).total;
+  return bwd_workspace<bf16_t>(n_seqs, tokens_q, tokens_k, heads_q, heads_kv, d);
+}
+size_t vmonarch_packed_attention_bwd_workspace_bytes_f32(int n_seqs, long long tokens_q, long long tokens_k, int heads_q, int heads_kv, int d) {
+  return bwd_workspace<float>(n_seqs, tokens_q, tokens_k, heads_q, heads_kv, d);
 }
 int vmonarch_packed_attention_bwd(const vmonarch_tokens* q, const vmonarch_tokens* k, const vmonarch_tokens* v, const vmonarch_tokens* out,
                                   const vmonarch_tokens* d_out, const float* lse, const vmonarch_tokens* dq, const vmonarch_tokens* dk,
