@@ -27,7 +27,7 @@ EXTRA = {"flash2.hip": ["-fno-honor-nans", "-Wno-inline-asm"],
          "flash_kv.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-fno-honor-nans"],
          "frame.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-fno-honor-nans"],
          "f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
-         "seq_mfma.hip": ["-fno-honor-nans", "-Wno-inline-asm"],
+         "seq_mfma.hip": ["-Wno-inline-asm"],
          "seq_token.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
          "seq_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
          "seq_general.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
