@@ -79,7 +79,8 @@ int vmonarch_rotary_scale(vmonarch_rotary_plan* plan, double factor, double cont
  * the pair's angle and the plan's amplitude; backward != 0: the transpose (sin a negated), which takes the gradient
  * of y to that of x.  k may be NULL (heads_k 0).  positions: DEVICE int32 [axes][tokens], row a at
  * positions + a * axis_stride.  Angles are reduced in 64 bits: any int32 position keeps full precision.
- * Outputs may be their inputs (same pointer and strides); otherwise nothing may overlap.  tokens == 0 is a no-op.
+ * Outputs may be their inputs (same pointer and strides); otherwise no output may overlap a tensor of the call (the same address is refused).
+ * tokens == 0 is a no-op.
  */
 int vmonarch_rotary(const vmonarch_tokens* q, const vmonarch_tokens* q_out, int heads_q, const vmonarch_tokens* k,
                     const vmonarch_tokens* k_out, int heads_k, long long tokens, int d, const int32_t* positions,

@@ -155,6 +155,8 @@ int rotary_impl(const vmonarch_tokens* q, const vmonarch_tokens* q_out, int head
   for (int x = 0; x < (k ? 2 : 1); ++x)
     if (in[x]->data == out[x]->data && (in[x]->token_stride != out[x]->token_stride || in[x]->head_stride != out[x]->head_stride))
       return api_fail(VMONARCH_ERR_INVALID_ARG, "an output in place of its input must have its strides");
+  if (k && tokens > 0 && (q_out->data == k_out->data || q_out->data == k->data || k_out->data == q->data))
+    return api_fail(VMONARCH_ERR_INVALID_ARG, "q_out and k_out must not be another tensor of the call");
   if (axis_stride < 0) return api_fail(VMONARCH_ERR_INVALID_ARG, "negative axis_stride");
   if (tokens == 0) return VMONARCH_OK;
   RotaryParams P = {};
