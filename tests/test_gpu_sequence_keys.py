@@ -194,3 +194,37 @@ def test_gradients_of_every_pair(B, dtype, d, kv, group, ql, kl, causal):  # noq
             size[:, :n] = w[:, cols] * 2
             assert ((dq[at:at + a].double() - want[:, None]).abs() <= (3 * half + 2.0 ** -16) * size[:, None]).all(), first
             at += a
+
+
+def test_a_table_cut_to_the_longest_sequence(B):  # noqa: F811
+    """Rows of a wide table, shown as wide as the sequences need: the calls of a table of just that width, ranges included, to the last bit."""
+    gen = torch.Generator().manual_seed(3)
+    have, new, page, kv, heads, d = [700, 65, 512], [1, 40, 3], 16, 2, 4, 128
+    ck, cv, tight = pages(gen, have, page, kv, d, "bf16")
+    need = -(-max(have) // page)
+    tight = tight[:, :need].contiguous()
+    wide = torch.full((len(have), 4096), -1, dtype=torch.int32, device="cuda")
+    wide[:, :need] = tight
+    lengths = torch.tensor(have, dtype=torch.int32, device="cuda")
+    B.paged_append(tokens(gen, sum(have), kv, d, "bf16"), tokens(gen, sum(have), kv, d, "bf16"), ck, cv, wide[:, :need], starts(have), lengths)
+    q = tokens(gen, sum(new), heads, d, "bf16")
+    for causal in (True, False):
+        out = B.paged_attention(q, ck, cv, wide[:, :need], starts(new), lengths, causal=causal)
+        assert torch.equal(out, B.paged_attention(q, ck, cv, tight, starts(new), lengths, causal=causal)) and torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("bf16", 136), ("f32", 64)])
+def test_no_keys_and_no_queries_at_all(B, dtype, d):  # noqa: F811
+    """A batch without a single key: rows of zeros, log-sum-exps of -inf, gradients of zero.  Without a single query: the keys' gradients are zero."""
+    gen = torch.Generator().manual_seed(d)
+    some, none = starts([30, 0, 140]), starts([0, 0, 0])
+    x = {h: tokens(gen, 170, h, d, dtype) for h in (4, 2)}
+    y = {h: tokens(gen, 0, h, d, dtype) for h in (4, 2)}
+    for causal in (True, False):
+        out, lse = B.packed_attention(x[4], y[2], y[2], some, none, causal=causal, lse=True)
+        assert (out == 0).all() and torch.isneginf(lse).all()
+        dq, dk, dv = B.packed_attention_bwd(x[4], y[2], y[2], out, x[4], lse, some, none, causal=causal)
+        assert (dq == 0).all() and dk.shape == dv.shape == (0, 2, d)
+        out, lse = B.packed_attention(y[4], x[2], x[2], none, some, causal=causal, lse=True)
+        dq, dk, dv = B.packed_attention_bwd(y[4], x[2], x[2], out, y[4], lse, none, some, causal=causal)
+        assert dq.shape == (0, 4, d) and (dk == 0).all() and (dv == 0).all()
