@@ -78,7 +78,8 @@ int vmonarch_rotary_scale(vmonarch_rotary_plan* plan, double factor, double cont
  * Turns every pair (x0, x1) of every head: y0 = A (x0 cos a - x1 sin a), y1 = A (x0 sin a + x1 cos a), a and A
  * the pair's angle and the plan's amplitude; backward != 0: the transpose (sin a negated), which takes the gradient
  * of y to that of x.  k may be NULL (heads_k 0).  positions: DEVICE int32 [axes][tokens], row a at
- * positions + a * axis_stride.  Angles are reduced in 64 bits: any int32 position keeps full precision.
+ * positions + a * axis_stride.  Angles are formed and reduced in 64 bits, to
+ * 2^-52 of themselves: below fp32's rounding up to 2^28 radians, 5e-7 at 2^31.
  * Outputs may be their inputs (same pointer and strides); otherwise no output may overlap a tensor of the call (the same address is refused).
  * tokens == 0 is a no-op.
  */
@@ -168,8 +169,10 @@ int vmonarch_paged_append_f32(const vmonarch_tokens* k, const vmonarch_tokens* v
 /*
  * Attention of each sequence's chunk of new tokens (or its single one) over its lengths[s] cached tokens, the chunk's own
  * included: vmonarch_packed_attention with the keys and values of sequence s taken from its pages.  Few rows over long caches are
- * cut into ranges of keys and joined by a second launch; the cut follows what the host knows (tokens, n_seqs, heads, the mask, the longest
- * sequence the table has room for), so the same sizes give the same bits.  workspace: DEVICE, 256-byte aligned, at least
+ * cut into ranges of keys and joined by a second launch; the cut, and with it the workspace, follows what the host knows (tokens, n_seqs, heads, the
+ * mask, the longest sequence the table has room for), so the same sizes give the same bits.  Of a table with room for far more than is there give
+ * the columns that the longest sequence needs (a smaller table_width at the same table_stride): its prompts are not cut then (8 of up to 2000 tokens, 12
+ * heads, d = 128: 144 us with room for 2000 to 8192 tokens, 324 for 32,768).  workspace: DEVICE, 256-byte aligned, at least
  * vmonarch_paged_attention_workspace_bytes(...) bytes (0: none needed), or NULL for the process-wide one.
  */
 size_t vmonarch_paged_attention_workspace_bytes(const vmonarch_cache* cache, int n_seqs, long long tokens, int heads_q,

@@ -605,7 +605,8 @@ def paged_append(k, v, cache_k, cache_v, table, q_starts, lengths, plan: RotaryP
 
 def paged_attention(q, cache_k, cache_v, table, q_starts, lengths, causal=True, scale=None, out=None, workspace=None):
     """Attention of each sequence's chunk of new tokens (q [tokens, heads_q, d], cut by q_starts) over its lengths[s] tokens in the pages, the chunk's
-    own included.  Rows of no sequence are not written (see packed_attention)."""
+    own included.  Rows of no sequence are not written (see packed_attention).  The table's width stands for the longest sequence where keys are cut into
+    ranges: of one with room for far more give the columns in use, table[:, :n]."""
     nq, heads, like = _sizes("q", q)
     d, _, dev = like
     n = q_starts.numel()

@@ -49,7 +49,7 @@ struct SeqParams {
   Rows<const E> o, d_out;
   Rows<E> dq, dk, dv;
   float* delta;         // per row: seq_general.hip d_out . out, [heads_q][tokens_q]; seq_bwd.hip see there
-  // ranges of keys (seq_paged.hip)
+  // ranges of keys (forward, pages) or of query rows (backward): partial results and their log-sums
   float* part_o;
   float* part_s;
   int ranges;

@@ -19,9 +19,10 @@
 // own would be two products).  For dq the sum is of the ROUNDED dS': the weights that the keys really
 // get add up to zero, so a row that sits on one key loses no digits to it, nor does what all keys have in common.  Errors of dq and dk stay at 1.2 to
 // 1.5 roundings of the result at any sharpness and length (with D' alone 2.7 to 4.4 at logit deviations of 8 and 16).
-// Bound by the matrix units and the LDS reads that feed them (an operand per MFMA): they are busy for 0.4 of the cycles, the vector units for as
+// Bound by the matrix units and the LDS reads that feed them (an operand per MFMA): they are busy for 0.50 (dQ) and 0.39 (dK, dV) of the cycles, the vector units for as
 // many, and two waves on a SIMD, all that the registers allow, overlap the two only in part.  3 x 4096 causal tokens, 12 heads on 4, d = 128: dQ
-// 214 us (849 TFLOP/s), dK and dV with their join 343 (705); forward and backward 643.  Operands requested further ahead, G and dP in turn, twice the rows
+// 274 us (883 TFLOP/s of the products issued), dK and dV with their join 340 (710), in single launches under a tracer; forward and backward in a row 679 to
+// 715 from card to card.  Operands requested further ahead, G and dP in turn, twice the rows
 // between barriers: level, or behind for spilled registers.
 #include "seq_device.h"
 
@@ -539,8 +540,8 @@ hipError_t launch(const SeqParams<bf16_t>& P, hipStream_t st) {
 
 // Ranges the rows of queries are cut into for dK and dV: up to three workgroups of 128 keys for every compute unit (which holds one), but none below
 // 512 rows of an average sequence.  Forward and backward, us by workgroups a unit, one / two / three / four: 3 x 4096 tokens, 12 heads on 4, d =
-// 128 692 / 691 / 659 / 661, without a mask 1185 / 1186 / 1137 / 1136; one sequence of 4096 532 / 396 / 390 / 402; 2 x 2000, 12 heads on 12 197 / 197 /
-// 197 / 256; 4 clips of up to 3157 rows on texts of up to 512 keys, 10 heads of 64 107 / 87 / 90 / 90.
+// 128 717 / 716 / 683 / 698, without a mask 1255 / 1255 / 1214 / 1209; one sequence of 4096 418 / 414 / 414 / 428; 2 x 2000, 12 heads on 12 202 / 202 /
+// 202 / 249; 4 clips of up to 3157 rows on texts of up to 512 keys, 10 heads of 64 108 / 90 / 93 / 93.
 int seq_bwd_ranges(int n_seqs, long long tokens_q, long long tokens_k, int heads_kv, int group) {
   const long long blocks = tile_bound(tokens_k, 1, 32 * NT, n_seqs) * heads_kv;
   long long r = 3LL * compute_units() / (blocks > 0 ? blocks : 1);

@@ -13,8 +13,8 @@
 // products of n - 1 dealt over the same instruction slots); the tiles at the end of the range that some row sees in part or
 // not at all (the diagonal, the ragged end) follow in plain order, with a true running maximum, masks, and a look at the values: zero times
 // infinity must not reach a row that does not see the key.
-// Bound by the matrix units, with the clock held down by power, where rows are many: 16,384 causal tokens, 12 heads on 4, 763 to 810 us at d =
-// 128 from card to card (1080 to 1018 TFLOP/s; a large library product reaches 1233), 433 to 446 at d = 64 (950).  The queries have to be waited for
+// Bound by the matrix units, with the clock held down by power, where rows are many: 16,384 causal tokens, 12 heads on 4, 763 to 811 us a call at d =
+// 128 from card to card (1080 to 1018 TFLOP/s; a large library product reaches 1233; 860 in single launches under a tracer), 433 to 446 at d = 64 (950).  The queries have to be waited for
 // in front of the loop: the compiler's own wait for them stood in it and took the tile just requested along (845 us in place of 763 on one card,
 // 107 in place of 87 for a frame over pages).  A lone workgroup takes 0.35 us per 32 keys at d = 64, 0.57 at 128, which bounds short prompts (a
 // dozen of up to 700 tokens: 17 us).  Level or behind: operands requested up to seven MFMAs ahead instead of three; keys and values requested three

@@ -18,7 +18,7 @@ namespace {
 
 constexpr int NW = 2;
 
-constexpr int NS = 2;  // sub-tiles in LDS per wave: 64 KB a workgroup at d = 128, half that at d = 64 (two and three workgroups on a unit)
+constexpr int NS = 2;  // sub-tiles in LDS per wave: 64 KB a workgroup at d = 128, half that at d = 64 (two and four workgroups on a unit)
 
 template <int D>
 __global__ void __launch_bounds__(64 * NW, D == 64 ? 3 : 2) seq_token_kernel(SeqParams<bf16_t> P) {
