@@ -18,11 +18,12 @@
 // at the cost of an eighth product, sum_j P k, on the operands of the first (3 x 4096 tokens forward and backward 652 -> 711 us; D summed in a round of its
 // own would be two products).  For dq the sum is of the ROUNDED dS': the weights that the keys really
 // get add up to zero, so a row that sits on one key loses no digits to it, nor does what all keys have in common.  Errors of dq and dk stay at 1.2 to
-// 1.5 roundings of the result at any sharpness and length (with D' alone 2.7 to 4.4 at logit deviations of 8 and 16).
+// 1.5 roundings of the result at any sharpness and length (with D' alone 2.7 to 4.4 at logit deviations of 8 and 16): the result's own and that of the
+// operands dS and P, which the bf16 matrix units take in eight bits.
 // Bound by the matrix units and the LDS reads that feed them (an operand per MFMA): they are busy for 0.50 (dQ) and 0.39 (dK, dV) of the cycles, the vector units for as
 // many, and two waves on a SIMD, all that the registers allow, overlap the two only in part.  3 x 4096 causal tokens, 12 heads on 4, d = 128: dQ
 // 274 us (883 TFLOP/s of the products issued), dK and dV with their join 340 (710), in single launches under a tracer; forward and backward in a row 679 to
-// 715 from card to card.  Operands requested further ahead, G and dP in turn, twice the rows
+// 717 from card to card.  Operands requested further ahead, G and dP in turn, twice the rows
 // between barriers: level, or behind for spilled registers.
 #include "seq_device.h"
 
